@@ -248,10 +248,11 @@ def _run_own(st):
     if kind == "read":
         return lr.cache_read(cache, dt)
     if kind == "append":
-        h = lr.cache_route_fwd(cache, st["K"], st["q"], c["mode"], EPS, o_new=st["o_new"])
+        h = lr.cache_route_fwd(cache, st["K"], st["q"], c["mode"], EPS, o_new=st["o_new"],
+                               dtype=dt)
         return (h, *_as_values(st)) if c["fmt"] == "fp8" else (h, lr.cache_read(cache.planes(-1), dt))
     if kind == "fwd":
-        return lr.cache_route_fwd(cache, st["K"], st["q"], c["mode"], EPS)
+        return lr.cache_route_fwd(cache, st["K"], st["q"], c["mode"], EPS, dtype=dt)
     if kind == "bwd":
         dV, dK, dq = lr.cache_route_bwd(cache, st["K"], st["q"], st["dH"], c["mode"], EPS)
         return (dV, dq) if dK is None else (dV, dK, dq)
