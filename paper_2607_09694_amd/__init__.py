@@ -105,6 +105,18 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
     lib.lr_attnres_key_proj_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, i64,
                                             i64, i64, i64, i, vp]
     lib.lr_attnres_key_proj_bwd.restype = ctypes.c_int
+    sz = ctypes.c_size_t
+    for name, args in (("write", [vp] * 3 + [i64, i64, i, i, vp]),
+                       ("read", [vp] * 3 + [i64, i64, i, i, vp]),
+                       ("route_fwd", [vp] * 6 + [i64] * 4 + [i, i, i, f, vp]),
+                       ("route_bwd", [vp] * 9 + [sz] + [i64] * 4 + [i, i, i, f, i, vp]),
+                       ("route_bwd_deferred", [vp] * 8 + [sz] + [i64] * 4 + [i, i, i, f, vp])):
+        fn = getattr(lib, f"lr_attnres_cache_{name}")
+        fn.argtypes, fn.restype = args, ctypes.c_int
+    for name, args in (("row_bytes", [i64, i]), ("row_scales", [i64]),
+                       ("route_bwd_workspace_bytes", [i64] * 4 + [i, i, i])):
+        fn = getattr(lib, f"lr_attnres_cache_{name}")
+        fn.argtypes, fn.restype = args, sz
     lib.lr_attnres_last_error.argtypes = []
     lib.lr_attnres_last_error.restype = ctypes.c_char_p
     lib.lr_attnres_abi_version.argtypes = []
@@ -763,3 +775,260 @@ def block_merge_fwd(B, KB, o_new, k_new, q, state, slot: int, start: bool, mode,
         N, d, r, mode, _dtype_code(o_new), float(eps), _stream(B))
     _check(lib, rc)
     return H
+
+
+# ---------------------------------------------------------------------------
+# The source stack in 8 or 4 bits (include/lr_attnres_cache.h)
+# ---------------------------------------------------------------------------
+
+FP8, FP4 = 0, 1
+FORMATS = {"fp8": FP8, "fp4": FP4}
+_CODE_BYTES = (32, 16)  # of a block of 32 columns
+
+
+class SourceCache:
+    """A stack of S sources of N rows and d columns held in blocks of 32 columns:
+    codes [S, N, 32 nb] ("fp8", e4m3) or [S, N, 16 nb] ("fp4", e2m1, the even
+    column in the low half) and one scale byte a block, scales [S, N, nb], uint8,
+    nb = ceil(d / 32); the byte e stands for 2^(e - 127), 255 for a block of NaN.
+    The tensors are the caller's (``source_cache`` makes them).
+    """
+
+    __slots__ = ("codes", "scales", "d", "fmt", "_shape")
+
+    def __init__(self, codes, scales, d: int, fmt="fp8"):
+        import torch
+
+        self.fmt = FORMATS[fmt] if isinstance(fmt, str) else int(fmt)
+        if self.fmt not in (FP8, FP4):
+            raise ValueError(f"unknown cache format {fmt}")
+        nb = -(-d // 32)
+        if d < 1 or codes.dim() != 3 or codes.shape[2] != nb * _CODE_BYTES[self.fmt] \
+                or tuple(scales.shape) != (codes.shape[0], codes.shape[1], nb):
+            raise ValueError(f"need codes [S, N, {nb * _CODE_BYTES[self.fmt]}] and scales "
+                             f"[S, N, {nb}] for rows of {d} columns")
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+            raise TypeError("codes and scales must be uint8")
+        self.codes, self.scales, self.d = codes, scales, int(d)
+        self._shape = (codes.shape[0], codes.shape[1], self.d)
+
+    @property
+    def shape(self):
+        """(S, N, d)."""
+        return self._shape
+
+    def planes(self, first: int, count: int = 1) -> "SourceCache":
+        """The sources first .. first + count - 1 (first < 0 counts from the end),
+        a view: a site of t sources reads ``planes(0, t)``."""
+        S = self._shape[0]
+        first = first + S if first < 0 else first
+        if not (0 <= first and 0 <= count and first + count <= S):
+            raise ValueError(f"planes {first} .. {first + count - 1} of {S}")
+        return SourceCache(self.codes[first:first + count], self.scales[first:first + count],
+                           self.d, self.fmt)
+
+
+def source_cache(S: int, N: int, d: int, fmt="fp8", device="cuda") -> SourceCache:
+    """An empty cache (all zeros) of S sources of N rows and d columns."""
+    import torch
+
+    f = FORMATS[fmt] if isinstance(fmt, str) else int(fmt)
+    nb = -(-d // 32)
+    return SourceCache(torch.zeros((S, N, nb * _CODE_BYTES[f]), dtype=torch.uint8, device=device),
+                       torch.ones((S, N, nb), dtype=torch.uint8, device=device), d, f)
+
+
+def _cache_args(cache):
+    return _dev(cache.codes, "codes"), _dev(cache.scales, "scales")
+
+
+def _cache_site(cache, K, q, mode, others):
+    """Shapes and devices of one read site over a cache; (S, N, d, r)."""
+    S, N, d = cache._shape
+    if mode == PROJECTED:
+        if K is None or K.dim() != 3 or K.shape[0] != S or K.shape[1] != N:
+            raise ValueError("K must be [S, N, r] for projected keys")
+    elif K is not None:
+        raise ValueError("K must be None unless keys are projected")
+    r = K.shape[2] if mode == PROJECTED else q.shape[0]
+    if q.dim() != 1 or q.shape[0] != r:
+        raise ValueError(f"q must have shape ({r},)")
+    _same_device(cache.codes, cache.scales, K, q, *others)
+    return S, N, d, r
+
+
+def _same_device(first, *others):
+    dev = first.device
+    for t in others:
+        if t is not None and t.device != dev:
+            raise ValueError(f"all tensors must be on {dev}, got one on {t.device}")
+
+
+def _shaped(t, shape, name):
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return t
+
+
+def _call(lib, fn, t, *args):
+    """fn(*args, stream) on t's device, whichever is current."""
+    import torch
+
+    index = t.get_device()
+    if index == torch.cuda.current_device():
+        _check(lib, fn(*args, _stream(t)))
+    else:
+        with torch.cuda.device(index):
+            _check(lib, fn(*args, _stream(t)))
+
+
+def cache_write(cache, O):
+    """Quantises O [S, N, d] bf16/fp32 into the cache's planes (one source as it
+    is written: ``cache_write(cache.planes(i), o[None])``).  Per block of 32
+    columns the power of two is the smallest for which nothing saturates; codes
+    round to nearest even; a block with a NaN or an infinity reads as NaN."""
+    lib = load_library()
+    S, N, d = cache._shape
+    _shaped(O, (S, N, d), "O")
+    _same_device(cache.codes, cache.scales, O)
+    codes, scales = _cache_args(cache)
+    _call(lib, lib.lr_attnres_cache_write, cache.codes, _dev(O, "O"), codes, scales, S * N, d,
+          cache.fmt, _dtype_code(O))
+
+
+def cache_read(cache, dtype=None, out=None):
+    """The values that the cache holds, [S, N, d] in ``dtype`` (default bf16):
+    exact in fp32 and, down to bf16's subnormals, in bf16."""
+    import torch
+
+    lib = load_library()
+    if out is None:
+        out = torch.empty(cache._shape, dtype=dtype or torch.bfloat16, device=cache.codes.device)
+    elif dtype is not None and out.dtype != dtype:
+        raise TypeError(f"out must be {dtype}, got {out.dtype}")
+    S, N, d = cache._shape
+    _shaped(out, (S, N, d), "out")
+    _same_device(cache.codes, cache.scales, out)
+    codes, scales = _cache_args(cache)
+    _call(lib, lib.lr_attnres_cache_read, cache.codes, codes, scales, _dev(out, "out"), S * N, d,
+          cache.fmt, _dtype_code(out))
+    return out
+
+
+def cache_route_fwd(cache, K, q, mode, eps: float = 1e-6, o_new=None, dtype=None, out=None):
+    """route_fwd over a cache: h[n] = sum_i alpha_i x_i[n] with x_i the values
+    that the cache holds (Eq. lr_attnres_output).
+
+    K [S,N,r] bf16/fp32 (projected) or None; q [r] fp32.  With ``o_new`` [N,d]
+    the newest source is first written into the last plane, as by cache_write,
+    and the site reads it as every later site will.  Returns H [N,d] in
+    ``dtype`` (default: that of ``out``, K or o_new, else bf16), which is also
+    that of K and o_new.
+    """
+    import torch
+
+    lib = load_library()
+    mode = _mode(mode)
+    S, N, d, r = _cache_site(cache, K, q, mode, (o_new, out))
+    if dtype is None:
+        dtype = next((t.dtype for t in (out, K, o_new) if t is not None), torch.bfloat16)
+    H = _shaped(out, (N, d), "out") if out is not None else torch.empty((N, d), dtype=dtype,
+                                                                      device=q.device)
+    if o_new is not None:
+        _shaped(o_new, (N, d), "o_new")
+    codes, scales = _cache_args(cache)
+    _call(lib, lib.lr_attnres_cache_route_fwd, cache.codes, codes, scales, _dev(K, "K", dtype),
+          _dev(q, "q", torch.float32), _dev(o_new, "o_new", dtype), _dev(H, "H", dtype), S, N, d,
+          r, mode, cache.fmt, _dtype_code(H), float(eps))
+    return H
+
+
+def cache_route_bwd_workspace_bytes(S, N, d, r, mode, fmt, dtype) -> int:
+    """Workspace bytes of cache_route_bwd and cache_route_bwd_deferred."""
+    import torch
+
+    code = _BF16 if dtype == torch.bfloat16 else _F32
+    f = FORMATS[fmt] if isinstance(fmt, str) else int(fmt)
+    return load_library().lr_attnres_cache_route_bwd_workspace_bytes(S, N, d, r, _mode(mode), f,
+                                                                     code)
+
+
+def _cache_workspace(lib, workspace, dH, S, N, d, r, mode, fmt, code):
+    import torch
+
+    if workspace is not None:
+        _same_device(dH, workspace)
+        return workspace
+    need = lib.lr_attnres_cache_route_bwd_workspace_bytes(S, N, d, r, mode, fmt, code)
+    return torch.empty((max(need, 16),), dtype=torch.uint8, device=dH.device)
+
+
+def cache_route_bwd(cache, K, q, dH, mode, eps: float = 1e-6, out=None, workspace=None,
+                    accumulate: bool = False):
+    """route_bwd from 8- or 4-bit checkpoints: gradients (dV, dK, dq) of
+    L = sum(dH * H) with respect to the values that the cache holds, which
+    training hands to the sources unchanged.
+
+    dH [N,d] bf16/fp32; dV [S,N,d] and dK [S,N,r] (projected keys, else None) in
+    its dtype; dq [r] fp32.  ``out`` may supply (dV, dK, dq), ``workspace`` a
+    device buffer of cache_route_bwd_workspace_bytes(...) bytes; with
+    ``accumulate`` the gradients are added into ``out``.
+    """
+    import torch
+
+    lib = load_library()
+    mode = _mode(mode)
+    dV, dK, dq = out if out is not None else (None, None, None)
+    S, N, d, r = _cache_site(cache, K, q, mode, (dH, dV, dK, dq))
+    _shaped(dH, (N, d), "dH")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs the out=(dV, dK, dq) buffers to add into")
+        dV = torch.empty((S, N, d), dtype=dH.dtype, device=dH.device)
+        dK = torch.empty_like(K) if mode == PROJECTED else None
+        dq = torch.empty((r,), dtype=torch.float32, device=dH.device)
+    else:
+        _shaped(dV, (S, N, d), "dV")
+        _shaped(dq, (r,), "dq")
+        if (dK is not None) != (mode == PROJECTED):
+            raise ValueError("dK must be given with projected keys and None otherwise")
+        if dK is not None:
+            _shaped(dK, (S, N, r), "dK")
+    code, dt = _dtype_code(dH), dH.dtype
+    workspace = _cache_workspace(lib, workspace, dH, S, N, d, r, mode, cache.fmt, code)
+    codes, scales = _cache_args(cache)
+    _call(lib, lib.lr_attnres_cache_route_bwd, dH, codes, scales, _dev(K, "K", dt),
+          _dev(q, "q", torch.float32), _dev(dH, "dH"), _dev(dV, "dV", dt), _dev(dK, "dK", dt),
+          _dev(dq, "dq", torch.float32), _dev(workspace, "workspace"),
+          workspace.numel() * workspace.element_size(), S, N, d, r, mode, cache.fmt, code,
+          float(eps), int(bool(accumulate)))
+    return dV, dK, dq
+
+
+def cache_route_bwd_deferred(cache, K, q, dH, mode, coef, eps: float = 1e-6, dq=None,
+                             workspace=None):
+    """route_bwd_deferred from 8- or 4-bit checkpoints: one site of the deferred
+    reverse pass.  Writes the coefficients of its S sources into coef [S,3,N]
+    fp32 (alpha, ds/rho, ds s/(rho r)) and returns its dq [r] fp32.
+    route_gather_bwd then forms each source's gradient; with sliced keys it
+    takes the source's plane from cache_read(cache.planes(i))."""
+    import torch
+
+    lib = load_library()
+    mode = _mode(mode)
+    S, N, d, r = _cache_site(cache, K, q, mode, (dH, coef, dq))
+    _shaped(dH, (N, d), "dH")
+    _shaped(coef, (S, 3, N), "coef")
+    if dq is None:
+        dq = torch.empty((r,), dtype=torch.float32, device=dH.device)
+    else:
+        _shaped(dq, (r,), "dq")
+    code = _dtype_code(dH)
+    workspace = _cache_workspace(lib, workspace, dH, S, N, d, r, mode, cache.fmt, code)
+    codes, scales = _cache_args(cache)
+    _call(lib, lib.lr_attnres_cache_route_bwd_deferred, dH, codes, scales,
+          _dev(K, "K", dH.dtype), _dev(q, "q", torch.float32), _dev(dH, "dH"),
+          _dev(coef, "coef", torch.float32), _dev(dq, "dq", torch.float32),
+          _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), S, N, d, r,
+          mode, cache.fmt, code, float(eps))
+    return dq

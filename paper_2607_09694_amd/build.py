@@ -12,7 +12,9 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "liblrattnres.so")
 SOURCES = ["route_fwd.hip", "route_bwd.hip", "route_bwd_defer.hip", "route_block.hip", "route_all.hip",
-           "route_all_bwd.hip", "route_all_wide.hip", "key_proj.hip", "key_proj_bwd.hip", "route_plan.cpp", "capi.cpp"]
+           "route_all_bwd.hip", "route_all_wide.hip", "key_proj.hip", "key_proj_bwd.hip",
+           "cache_store.hip", "cache_fwd.hip", "cache_bwd_fp8.hip", "cache_bwd_fp4.hip",
+           "cache_plan.cpp", "route_plan.cpp", "capi.cpp"]
 # Benchmark-only helper: streaming copy / read kernels of known traffic.
 PROBE_LIB = os.path.join(PKG, "libhbmprobe.so")
 PROBE_SOURCES = ["hbm_probe.hip"]

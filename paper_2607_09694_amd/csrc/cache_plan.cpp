@@ -1,0 +1,53 @@
+// Layout of the backward over a source stack in 8 or 4 bits, its workspace, and
+// its launch.  Host code only.
+#include <algorithm>
+
+#include "cache_bwd.h"
+
+namespace lrar {
+
+namespace {
+
+// Tokens up to which the low-rank backward splits each token's sources over a
+// workgroup, from this many sources on.
+constexpr int64_t kSplitBwd = 512;
+constexpr int64_t kSplitBwdSources = 9;
+
+}  // namespace
+
+CacheBwdPlan cache_bwd_plan(const CacheProblem &p)
+{
+    CacheBwdPlan pl;
+    const bool full = p.mode == LRAR_MODE_FULL;
+    pl.split = !full && p.N <= kSplitBwd && p.S >= kSplitBwdSources;
+    pl.tpw = full && p.N >= 4096 ? 4 : 1;
+    const int64_t per = pl.split ? 1 : (int64_t)kWaves * pl.tpw;
+    pl.nblocks = (int)((p.N + per - 1) / per);
+    return pl;
+}
+
+// Rows of dq partials.  Of a site of many sources: few may need fewer (their
+// tokens are not split), but a buffer sized for one site of a pass serves all.
+size_t cache_bwd_workspace_bytes(const CacheProblem &p)
+{
+    CacheProblem q = p;
+    q.S = std::max(p.S, kSplitBwdSources);
+    return (size_t)cache_bwd_plan(q).nblocks * (size_t)p.r * sizeof(float);
+}
+
+int launch_cache_bwd(const CacheProblem &p, const void *dH, void *dV, void *dK, float *coef,
+                     float *dq, void *ws, bool accumulate, hipStream_t st, std::string *err)
+{
+    float *partial = static_cast<float *>(ws);
+    hipError_t e = hipSuccess;
+    if (p.N > 0)
+        e = p.format == LRAR_CACHE_FP8
+                ? launch_cache_bwd_fp8(p, dH, dV, dK, coef, partial, accumulate, st)
+                : launch_cache_bwd_fp4(p, dH, dV, dK, coef, partial, accumulate, st);
+    if (e == hipSuccess)
+        e = launch_dq_reduce(partial, dq, p.N > 0 ? cache_bwd_plan(p).nblocks : 0, (int)p.r,
+                             accumulate, st);
+    return hip_status(e, "cache_route_bwd launch", err);
+}
+
+}  // namespace lrar

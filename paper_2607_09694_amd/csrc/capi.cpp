@@ -7,7 +7,9 @@
 
 #include <string>
 
+#include "cache_launch.h"
 #include "lr_attnres.h"
+#include "lr_attnres_cache.h"
 #include "route_launch.h"
 
 namespace {
@@ -963,6 +965,268 @@ int lr_attnres_block_gather_bwd(const float *B, const float *KB, int64_t slot, c
     if ((rc = lrar::launch_block_gather(g, static_cast<hipStream_t>(stream), &why)))
         return fail(rc, why);
     return LRAR_OK;
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// The source stack in 8 or 4 bits (lr_attnres_cache.h)
+// ---------------------------------------------------------------------------
+
+namespace {
+
+constexpr int64_t kMaxCacheRows = (int64_t)1 << 40, kMaxCacheWidth = (int64_t)1 << 20;
+
+int check_format(int format)
+{
+    if (format != LRAR_CACHE_FP8 && format != LRAR_CACHE_FP4)
+        return fail(LRAR_EINVAL, "unknown cache format " + std::to_string(format));
+    return LRAR_OK;
+}
+
+// Bytes of the codes and scales of `rows` rows.
+int cache_bytes(int64_t rows, int64_t d, int format, int64_t *codes, int64_t *scales)
+{
+    if (d > INT64_MAX - lrar::kCacheBlock || !mul_ok(rows, lrar::cache_blocks(d), scales) ||
+        !mul_ok(*scales, format == LRAR_CACHE_FP8 ? 32 : 16, codes))
+        return fail(LRAR_EINVAL, "tensor size overflows int64");
+    return LRAR_OK;
+}
+
+// No exception leaves the library.
+template <typename F> int guarded(F &&f)
+{
+    try {
+        g_last_error.clear();
+        return f();
+    } catch (...) {
+        return LRAR_EHIP;
+    }
+}
+
+// write: O to codes and scales; else the other way.
+int cache_copy(const void *O, const void *codes, const void *scales, int64_t rows, int64_t d,
+               int format, int dtype, bool write, void *stream)
+{
+    int rc;
+    if ((rc = check_format(format)))
+        return rc;
+    if (dtype != LRAR_DTYPE_F32 && dtype != LRAR_DTYPE_BF16)
+        return fail(LRAR_EINVAL, "unknown storage type " + std::to_string(dtype));
+    if (rows < 0 || d < 1)
+        return fail(LRAR_EINVAL, "sizes must satisfy rows >= 0, d >= 1");
+    const int64_t es = dtype == LRAR_DTYPE_BF16 ? 2 : 4;
+    int64_t cb, sb, ne, ob;
+    if ((rc = cache_bytes(rows, d, format, &cb, &sb)))
+        return rc;
+    if (!mul_ok(rows, d, &ne) || !mul_ok(ne, es, &ob))
+        return fail(LRAR_EINVAL, "tensor size overflows int64");
+    const bool data = rows > 0;
+    if ((rc = check_ptr(O, "O", (size_t)es, data)) || (rc = check_ptr(codes, "codes", 16, data)) ||
+        (rc = check_ptr(scales, "scales", 1, data)))
+        return rc;
+    const Span o[] = {span("O", O, ob)};
+    const Span c[] = {span("codes", codes, cb), span("scales", scales, sb)};
+    if ((rc = write ? check_aliasing(c, 2, o, 1) : check_aliasing(o, 1, c, 2)))
+        return rc;
+    if (rows > kMaxCacheRows || d > kMaxCacheWidth)
+        return fail(LRAR_EUNSUPPORTED, "more than 2^40 rows or 2^20 columns");
+    std::string why;
+    uint8_t *cp = static_cast<uint8_t *>(const_cast<void *>(codes));
+    uint8_t *sp = static_cast<uint8_t *>(const_cast<void *>(scales));
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    rc = write ? lrar::launch_cache_write(O, cp, sp, rows, d, format, dtype, st, &why)
+               : lrar::launch_cache_read(cp, sp, const_cast<void *>(O), rows, d, format, dtype, st,
+                                         &why);
+    return rc ? fail(rc, why) : LRAR_OK;
+}
+
+// The checks that the forward and both backwards share, and the sizes in bytes.
+struct CacheSizes {
+    int64_t codes, scales, k, h, v;
+};
+
+int check_cache_site(const void *codes, const void *scales, const void *K, const float *q,
+                     int64_t S, int64_t N, int64_t d, int64_t r, int mode, int format, int dtype,
+                     float eps, CacheSizes *z)
+{
+    int64_t ve, ke, he, rows;
+    int rc;
+    if ((rc = check_format(format)) || (rc = check_shape(S, N, d, r, mode, dtype, eps, &ve, &ke, &he)))
+        return rc;
+    if (!mul_ok(S, N, &rows))
+        return fail(LRAR_EINVAL, "tensor size overflows int64");
+    if ((rc = cache_bytes(rows, d, format, &z->codes, &z->scales)))
+        return rc;
+    const bool data = N > 0;
+    const bool proj = mode == LRAR_MODE_PROJECTED;
+    if ((rc = check_ptr(codes, "codes", 16, data)) || (rc = check_ptr(scales, "scales", 1, data)) ||
+        (rc = check_ptr(q, "q", 4, true)) || (rc = check_ptr(K, "K", 16, data && proj)))
+        return rc;
+    if (!proj && K)
+        return fail(LRAR_EINVAL, "K must be NULL unless keys are projected");
+    const int64_t es = dtype == LRAR_DTYPE_BF16 ? 2 : 4;
+    z->k = ke * es;
+    z->h = he * es;
+    z->v = ve * es;
+    return LRAR_OK;
+}
+
+lrar::CacheProblem cache_problem(const void *codes, const void *scales, const void *K,
+                                 const float *q, int64_t S, int64_t N, int64_t d, int64_t r,
+                                 int mode, int format, int dtype, float eps)
+{
+    return lrar::CacheProblem{static_cast<const uint8_t *>(codes),
+                              static_cast<const uint8_t *>(scales), K, q, S, N, d, r, mode, format,
+                              dtype, eps};
+}
+
+// coef NULL: the gradient rows; else the deferred form.
+int cache_bwd(const void *codes, const void *scales, const void *K, const float *q, const void *dH,
+              void *dV, void *dK, float *coef, bool deferred, float *dq, void *workspace,
+              size_t workspace_bytes, int64_t S, int64_t N, int64_t d, int64_t r, int mode,
+              int format, int dtype, float eps, bool accumulate, void *stream)
+{
+    CacheSizes z;
+    int rc = check_cache_site(codes, scales, K, q, S, N, d, r, mode, format, dtype, eps, &z);
+    if (rc)
+        return rc;
+    const bool data = N > 0;
+    const bool proj = mode == LRAR_MODE_PROJECTED;
+    if ((rc = check_ptr(dH, "dH", 16, data)) || (rc = check_ptr(dq, "dq", 4, true)) ||
+        (rc = check_ptr(dV, "dV", 16, data && !deferred)) ||
+        (rc = check_ptr(dK, "dK", 16, data && proj && !deferred)) ||
+        (rc = check_ptr(coef, "coef", 4, data && deferred)) ||
+        (rc = check_ptr(workspace, "workspace", 16, false)))
+        return rc;
+    if (!proj && dK)
+        return fail(LRAR_EINVAL, "K and dK must be NULL unless keys are projected");
+    const lrar::CacheProblem p = cache_problem(codes, scales, K, q, S, N, d, r, mode, format,
+                                               dtype, eps);
+    std::string why;
+    if ((rc = lrar::check_cache_supported(p, true, &why)))
+        return fail(rc, why);
+    if (deferred && mode == LRAR_MODE_FULL)
+        return fail(LRAR_EUNSUPPORTED, "the deferred backward takes projected or sliced keys");
+    const size_t need = lrar::cache_bwd_workspace_bytes(p);
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return fail(LRAR_EINVAL, "workspace too small: need " + std::to_string(need) + " bytes");
+    int64_t cf;
+    if (!mul_ok(S * N, 12, &cf))
+        return fail(LRAR_EINVAL, "tensor size overflows int64");
+    const Span outs[] = {span("dV", dV, z.v), span("dK", dK, z.k), span("coef", coef, cf),
+                         span("dq", dq, r * 4), span("workspace", workspace, (int64_t)need)};
+    const Span ins[] = {span("codes", codes, z.codes), span("scales", scales, z.scales),
+                        span("K", K, z.k), span("q", q, r * 4), span("dH", dH, z.h)};
+    if ((rc = check_aliasing(outs, 5, ins, 5)))
+        return rc;
+    rc = lrar::launch_cache_bwd(p, dH, dV, dK, coef, dq, workspace, accumulate,
+                                static_cast<hipStream_t>(stream), &why);
+    return rc ? fail(rc, why) : LRAR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lr_attnres_cache_row_bytes(int64_t d, int format)
+{
+    if (d < 1 || d > kMaxCacheWidth || (format != LRAR_CACHE_FP8 && format != LRAR_CACHE_FP4))
+        return 0;
+    return (size_t)lrar::cache_row_bytes(d, format);
+}
+
+size_t lr_attnres_cache_row_scales(int64_t d)
+{
+    return d < 1 || d > kMaxCacheWidth ? 0 : (size_t)lrar::cache_blocks(d);
+}
+
+int lr_attnres_cache_write(const void *O, void *codes, void *scales, int64_t rows, int64_t d,
+                           int format, int dtype, void *stream)
+{
+    return guarded([&] { return cache_copy(O, codes, scales, rows, d, format, dtype, true, stream); });
+}
+
+int lr_attnres_cache_read(const void *codes, const void *scales, void *O, int64_t rows, int64_t d,
+                          int format, int dtype, void *stream)
+{
+    return guarded([&] { return cache_copy(O, codes, scales, rows, d, format, dtype, false, stream); });
+}
+
+int lr_attnres_cache_route_fwd(void *codes, void *scales, const void *K, const float *q,
+                               const void *o_new, void *H, int64_t S, int64_t N, int64_t d,
+                               int64_t r, int mode, int format, int dtype, float eps,
+                               void *stream)
+{
+    return guarded([&]() -> int {
+        CacheSizes z;
+        int rc = check_cache_site(codes, scales, K, q, S, N, d, r, mode, format, dtype, eps, &z);
+        if (rc)
+            return rc;
+        if ((rc = check_ptr(H, "H", 16, N > 0)) || (rc = check_ptr(o_new, "o_new", 16, false)))
+            return rc;
+        // With o_new the newest plane is rewritten: nothing else may overlap the cache.
+        const Span outs[] = {span("H", H, z.h), span("codes", codes, z.codes),
+                             span("scales", scales, z.scales)};
+        const Span ins[] = {span("K", K, z.k), span("q", q, r * 4), span("o_new", o_new, z.h)};
+        if ((rc = check_aliasing(outs, 3, ins, 3)))
+            return rc;
+        const lrar::CacheProblem p = cache_problem(codes, scales, K, q, S, N, d, r, mode, format,
+                                                   dtype, eps);
+        std::string why;
+        if ((rc = lrar::check_cache_supported(p, false, &why)))
+            return fail(rc, why);
+        rc = lrar::launch_cache_fwd(p, o_new, H, static_cast<hipStream_t>(stream), &why);
+        return rc ? fail(rc, why) : LRAR_OK;
+    });
+}
+
+size_t lr_attnres_cache_route_bwd_workspace_bytes(int64_t S, int64_t N, int64_t d, int64_t r,
+                                                  int mode, int format, int dtype)
+{
+    try {
+        int64_t ve, ke, he;
+        const std::string saved = g_last_error;
+        int rc = check_format(format);
+        if (!rc)
+            rc = check_shape(S, N, d, r, mode, dtype, 0.0f, &ve, &ke, &he);
+        const lrar::CacheProblem p = cache_problem(nullptr, nullptr, nullptr, nullptr, S, N, d, r,
+                                                   mode, format, dtype, 0.0f);
+        std::string why;
+        if (!rc)
+            rc = lrar::check_cache_supported(p, true, &why);
+        g_last_error = saved;
+        return rc ? 0 : lrar::cache_bwd_workspace_bytes(p);
+    } catch (...) {
+        return 0;
+    }
+}
+
+int lr_attnres_cache_route_bwd(const void *codes, const void *scales, const void *K,
+                               const float *q, const void *dH, void *dV, void *dK, float *dq,
+                               void *workspace, size_t workspace_bytes, int64_t S, int64_t N,
+                               int64_t d, int64_t r, int mode, int format, int dtype, float eps,
+                               int accumulate, void *stream)
+{
+    return guarded([&]() -> int {
+        if (accumulate != 0 && accumulate != 1)
+            return fail(LRAR_EINVAL, "accumulate must be 0 or 1");
+        return cache_bwd(codes, scales, K, q, dH, dV, dK, nullptr, false, dq, workspace,
+                         workspace_bytes, S, N, d, r, mode, format, dtype, eps, accumulate != 0,
+                         stream);
+    });
+}
+
+int lr_attnres_cache_route_bwd_deferred(const void *codes, const void *scales, const void *K,
+                                        const float *q, const void *dH, float *coef, float *dq,
+                                        void *workspace, size_t workspace_bytes, int64_t S,
+                                        int64_t N, int64_t d, int64_t r, int mode, int format,
+                                        int dtype, float eps, void *stream)
+{
+    return guarded([&] {
+        return cache_bwd(codes, scales, K, q, dH, nullptr, nullptr, coef, true, dq, workspace,
+                         workspace_bytes, S, N, d, r, mode, format, dtype, eps, false, stream);
+    });
 }
 
 }  // extern "C"
