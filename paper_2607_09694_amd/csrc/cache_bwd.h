@@ -7,9 +7,8 @@
 //     columns),  dk_i = (ds_i / rho_i)(q - k_i s_i / (rho_i^2 r)),
 //     dq = sum ds_i k_i / rho_i,
 // the weights recomputed from the keys.  The stack is read once (full rank:
-// twice), in lanes of 16 columns; dV, which does not depend on it beyond the
-// key columns, is written from dH alone in lanes of 8 columns, whole lines a
-// wave.
+// twice) in the units of a lane; dV, which does not depend on it beyond the key
+// columns, is written from dH alone in lanes of 8 columns, whole lines a wave.
 #pragma once
 
 #include "cache_device.h"
@@ -19,171 +18,91 @@ namespace lrar {
 // What the backward of one site writes per source.
 enum CacheGrad { kGradWrite, kGradAdd, kGradCoef };
 
-// dq partials of the workgroup: the waves' shares in wave order.
-__device__ __forceinline__ void store_dq_partial(const float *stage, int stride,
-                                                 float *__restrict__ partial, int bx, int r)
+// dH in the units of a lane.
+template <int FMT, typename T, int LG, int NCH>
+__device__ __forceinline__ void load_dh(const T *__restrict__ row, const Lanes<FMT, LG, NCH> &ln, int d,
+                                        float (&dh)[NCH][UnitRaw<FMT>::cols])
 {
-    __syncthreads();
-    for (int j = threadIdx.x; j < r; j += kBlock) {
-        float sum = 0.0f;
-        for (int w = 0; w < kWaves; ++w)
-            sum += stage[w * stride + j];
-        partial[(size_t)bx * r + j] = sum;
-    }
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+        for (int h = 0; h < unit_cols<FMT>() / 8; ++h) {
+            float y[8];
+            load8(row, ln.col(c) + 8 * h, d, d % 8 == 0, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                dh[c][8 * h + e] = y[e];
+        }
 }
 
-// Projected / sliced keys.  A wave owns tpw tokens in turn; or (SPLIT, few
-// tokens) a workgroup owns one token, its sources cut into kWaves ranges, and
-// the scores and dots meet in LDS.
-template <int FMT, typename T, int NCH, bool SLICED, CacheGrad OUT, bool SPLIT>
-__global__ void __launch_bounds__(kBlock)
-cache_bwd_lr(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
-             const void *__restrict__ K, const float *__restrict__ q, const T *__restrict__ dH,
-             T *__restrict__ dV, T *__restrict__ dK, float *__restrict__ coef,
-             float *__restrict__ partial, int S, int N, int d, int r, float eps, int s_pad,
-             int r_pad, int tpw)
+// A lane's share of dH . x.
+template <int FMT>
+__device__ __forceinline__ float dot_unit(const UnitRaw<FMT> &w, const float (&dh)[UnitRaw<FMT>::cols],
+                                          float p)
 {
-    extern __shared__ float lds[];
-    const int lane = threadIdx.x & (kWaveSize - 1);
-    const int wave = threadIdx.x / kWaveSize;
-    const int slice = SPLIT ? 0 : 4 * wave;  // s, rho, g of the workgroup when split
-    float *s = lds + (slice + 0) * s_pad;
-    float *rho = lds + (slice + 1) * s_pad;
-    float *g = lds + (slice + 2) * s_pad;
-    float *alpha = lds + (slice + 3 + (SPLIT ? wave : 0)) * s_pad;
-    float *stage = lds + 4 * kWaves * s_pad;  // [kWaves][r_pad]
-    const int per = SPLIT ? (S + kWaves - 1) / kWaves : S;
-    const int ib = SPLIT ? min(S, wave * per) : 0, ie = SPLIT ? min(S, ib + per) : S;
-    auto meet = [&]() {
-        if constexpr (SPLIT)
-            __syncthreads();
-        else
-            wave_lds_sync();
-    };
+#pragma unroll
+    for (int h = 0; h < unit_cols<FMT>() / 16; ++h) {
+        float x[16];
+        unit_values<FMT>(w, h, x);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            p = fmaf(dh[16 * h + e], x[e], p);
+    }
+    return p;
+}
 
-    const Keys<FMT, T, SLICED> keys(K, codes, scales, N, d, r);
+// The key gradients of sources [ib, ie) of one token, dq included: lanes over
+// (source, key slot).  s, ri = 1 / rho, ds and alpha are the token's.
+template <int FMT, typename T, bool SLICED, CacheGrad OUT>
+__device__ __forceinline__ void key_grads(const Keys<FMT, T, SLICED> &keys, const T *__restrict__ dhrow,
+                                          T *__restrict__ dV, T *__restrict__ dK, const float (&qk)[8],
+                                          int ib, int ie, int n, int lane, const float *s,
+                                          const float *ri, const float *ds, const float *alpha,
+                                          float (&dq_acc)[8])
+{
+    typedef Keys<FMT, T, SLICED> Key;
+    constexpr int KP = 2;
     const int lps = keys.lps, spi = kWaveSize / lps;
     const int isub = lane / lps, v = lane % lps;
-    const int nb = (d + kCacheBlock - 1) / kCacheBlock;
-    const int wend = SLICED ? keys.base : d;  // columns [0, wend) of dV are alpha dH alone
-    const bool vec = d % 8 == 0;
-    const float inv_r = 1.0f / (float)r;
-    float qk[8], dq_acc[8];
-    keys.query(q, v, qk);
+    const float inv_r = 1.0f / (float)keys.r;
+    const bool vec = keys.d % 8 == 0;
+    float dhk[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        dq_acc[e] = 0.0f;
-
-    const int bx = blockIdx.x;
-    for (int t = 0; t < tpw; ++t) {
-        const int n = SPLIT ? bx : (bx * tpw + t) * kWaves + wave;
-        if (n >= N)
-            break;  // wave-uniform; the barrier below is outside the loop (SPLIT: n < N)
-        const T *dhrow = dH + (size_t)n * d;
-        if (ie > ib)
-            cache_scores<FMT, T, SLICED, 1>(keys, q, ib, ie, n, eps, lane, s, rho, s_pad);
-        meet();
-        depth_softmax<true>(s, alpha, S, lane);
-
-        // The dots of dH with the stored rows.
-        {
-            float dh[NCH][16];
+        dhk[e] = 0.0f;
+    if (SLICED && OUT != kGradCoef && v < keys.nkv)
+        load8(dhrow, keys.base + v * 8, keys.d, vec, dhk);
+    for (int i0 = ib; i0 < ie; i0 += KP * spi) {
+        typename Key::Raw w[KP];
 #pragma unroll
-            for (int c = 0; c < NCH; ++c)
+        for (int p = 0; p < KP; ++p)
+            if (p == 0 || i0 + p * spi < ie)  // wave-uniform
+                keys.load(min(i0 + p * spi + isub, ie - 1), n, v, w[p]);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float y[8];
-                    load8(dhrow, lane * kCacheVec + c * 1024 + 8 * h, d, vec, y);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        dh[c][8 * h + e] = y[e];
-                }
-            constexpr int U = NCH >= 4 ? 2 : 4;
-            for (int i0 = ib; i0 < ie; i0 += 8) {
-                float part[8];
-#pragma unroll
-                for (int h = 0; h < 8; h += U) {
-                    RowRaw<FMT> w[U][NCH];
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-#pragma unroll
-                        for (int c = 0; c < NCH; ++c)
-                            load_row<FMT>(codes, scales, (size_t)min(i0 + h + u, ie - 1) * N + n,
-                                          nb, RowAt<FMT>(lane * kCacheVec + c * 1024, nb),
-                                          w[u][c]);
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        float p = 0.0f;
-#pragma unroll
-                        for (int c = 0; c < NCH; ++c) {
-                            float x[16];
-                            row_values<FMT>(w[u][c], x);
-#pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                p = fmaf(dh[c][e], x[e], p);
-                        }
-                        part[h + u] = p;
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                const float tot = multi_sum<8>(part, lane);
-                const int idx = multi_sum_index<8>(lane);
-                if (multi_sum_writer<8>(lane) && i0 + idx < ie)
-                    g[i0 + idx] = tot;
-            }
-        }
-        meet();
-        float gb = 0.0f;
-        for (int i = lane; i < S; i += kWaveSize)
-            gb = fmaf(alpha[i], g[i], gb);
-        gb = wave_sum_t<true>(gb);
-        if constexpr (SPLIT)
-            meet();  // every wave has read the dots
-        for (int i = ib + lane; i < ie; i += kWaveSize)
-            g[i] = alpha[i] * (g[i] - gb);  // g now holds ds
-        wave_lds_sync();
-
-        // Key gradients: lanes over (source, key slot).
-        float dhk[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            dhk[e] = 0.0f;
-        if (SLICED && OUT != kGradCoef && v < keys.nkv)
-            load8(dhrow, keys.base + v * 8, d, vec, dhk);
-        for (int i0 = ib; i0 < ie; i0 += spi) {
-            const int i = i0 + isub;
+        for (int p = 0; p < KP; ++p) {
+            const int i = i0 + p * spi + isub;
             if (v >= keys.nkv || i >= ie)
                 continue;
-            typename Keys<FMT, T, SLICED>::Raw w;
-            float x[8];
-            keys.load(i, n, v, w);
-            keys.values(w, v, x);
-            const size_t row = (size_t)i * N + n;
-            const float ri = 1.0f / rho[i];
-            const float dsi = g[i];
-            const float cq = dsi * ri;           // ds_i / rho_i
+            float x[8], y[8];
+            keys.values(w[p], v, x);
+            const size_t row = (size_t)i * keys.N + n;
+            const float rv = ri[i], dsi = ds[i];
+            const float cq = dsi * rv;           // ds_i / rho_i
             const float ck = cq * s[i] * inv_r;  // ds_i s_i / (rho_i r)
-            if (OUT == kGradCoef && v == 0) {
-                coef[((size_t)i * 3 + 0) * N + n] = alpha[i];
-                coef[((size_t)i * 3 + 1) * N + n] = cq;
-                coef[((size_t)i * 3 + 2) * N + n] = ck;
-            }
-            float y[8];
             const float a = SLICED ? alpha[i] : 0.0f;
             const int j = keys.first(v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float kb = x[e] * ri;
+                const float kb = x[e] * rv;
                 dq_acc[e] = fmaf(dsi, kb, dq_acc[e]);
                 y[e] = a * dhk[e];
-                if (j + e >= 0)
+                if (!SLICED || j + e >= 0)
                     y[e] += fmaf(cq, qk[e], -ck * kb);
             }
             if constexpr (OUT != kGradCoef) {
-                T *orow = SLICED ? dV + row * d : dK + row * r;
+                T *orow = SLICED ? dV + row * keys.d : dK + row * keys.r;
                 const int ocol = SLICED ? keys.base + v * 8 : v * 8;
-                const int width = SLICED ? d : r;
+                const int width = SLICED ? keys.d : keys.r;
                 const bool ovec = SLICED ? vec : keys.vec;
                 if constexpr (OUT == kGradAdd) {
                     float o[8];
@@ -195,217 +114,463 @@ cache_bwd_lr(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scal
                 store8<T, false>(orow, ocol, width, ovec, y);
             }
         }
-
-        // dV_i = alpha_i dH before the key columns.
-        if constexpr (OUT != kGradCoef) {
-            constexpr int NO = 2 * NCH;  // chunks of 512 columns
-            float dh[NO][8];
-#pragma unroll
-            for (int c = 0; c < NO; ++c)
-                load8(dhrow, lane * 8 + c * 512, d, vec, dh[c]);
-            for (int i = ib; i < ie; ++i) {
-                const float a = alpha[i];
-                T *orow = dV + ((size_t)i * N + n) * d;
-#pragma unroll
-                for (int c = 0; c < NO; ++c) {
-                    const int col = lane * 8 + c * 512;
-                    float y[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        y[e] = a * dh[c][e];
-                    if constexpr (OUT == kGradAdd) {
-                        float o[8];
-                        load8(orow, col, wend, vec, o);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            y[e] += o[e];
-                    }
-                    store8<T, true>(orow, col, wend, vec, y);
-                }
-            }
-        }
-        wave_lds_sync();  // LDS of this token is reused by the next one
     }
+}
 
-    // dq: over the source groups of the wave, then over the waves.
+// dV_i = alpha_i dH of sources [ib, ie) of one token, columns [0, wend).
+template <typename T, int NO, CacheGrad OUT>
+__device__ __forceinline__ void value_grads(const T *__restrict__ dhrow, T *__restrict__ dV, int ib,
+                                            int ie, int n, int N, int d, int wend, int lane,
+                                            const float *alpha)
+{
+    const bool vec = d % 8 == 0;
+    float dh[NO][8];
+#pragma unroll
+    for (int c = 0; c < NO; ++c)
+        load8(dhrow, lane * 8 + c * 512, d, vec, dh[c]);
+    for (int i = ib; i < ie; ++i) {
+        const float a = alpha[i];
+        T *orow = dV + ((size_t)i * N + n) * d;
+#pragma unroll
+        for (int c = 0; c < NO; ++c) {
+            const int col = lane * 8 + c * 512;
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                y[e] = a * dh[c][e];
+            if constexpr (OUT == kGradAdd) {
+                float o[8];
+                load8(orow, col, wend, vec, o);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    y[e] += o[e];
+            }
+            store8<T, kBwdNtStore>(orow, col, wend, vec, y);
+        }
+    }
+}
+
+// The workgroup's dq: over the source groups of each wave (lanes of the same
+// key slot), then over the waves in order, into partial[bx][r].
+template <int FMT, typename T, bool SLICED>
+__device__ __forceinline__ void store_dq(const Keys<FMT, T, SLICED> &keys, float (&dq_acc)[8],
+                                         float *stage, int r_pad, float *__restrict__ partial, int bx,
+                                         int wave, int lane)
+{
+    const int v = lane % keys.lps, r = keys.r;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        for (int m = lps; m < kWaveSize; m <<= 1)
+        for (int m = keys.lps; m < kWaveSize; m <<= 1)
             dq_acc[e] += __shfl_xor(dq_acc[e], m, kWaveSize);
     float *my = stage + wave * r_pad;
-    if (isub == 0 && v < keys.nkv) {
+    if (lane / keys.lps == 0 && v < keys.nkv) {
         const int j = keys.first(v);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             if (j + e >= 0 && j + e < r)
                 my[j + e] = dq_acc[e];
     }
-    store_dq_partial(stage, r_pad, partial, bx, r);
+    __syncthreads();
+    for (int j = threadIdx.x; j < r; j += kBlock) {
+        float sum = 0.0f;
+        for (int w = 0; w < kWaves; ++w)
+            sum += stage[w * r_pad + j];
+        partial[(size_t)bx * r + j] = sum;
+    }
+}
+
+// The coefficients of P tokens from n0 on and sources [ib, ie), by `nthreads`
+// threads, runs of adjacent tokens together: coef[i][0..2][n] = alpha, ds / rho,
+// ds s / (rho r).  The token rows in LDS are s_pad apart (odd: no bank conflict).
+__device__ __forceinline__ void store_coef(float *__restrict__ coef, const float *s, const float *ri,
+                                           const float *ds, const float *alpha, int s_pad, int P,
+                                           int n0, int ib, int ie, int N, float inv_r, int thread,
+                                           int nthreads)
+{
+    const int count = min(P, N - n0);
+    for (int k = thread; k < P * (ie - ib); k += nthreads) {
+        const int t = k % P, i = ib + k / P;
+        if (t >= count)
+            continue;
+        const int at = t * s_pad + i;
+        const float cq = ds[at] * ri[at];
+        float *c = coef + (size_t)i * 3 * N + n0 + t;
+        c[0] = alpha[at];
+        c[N] = cq;
+        c[2 * (size_t)N] = cq * s[at] * inv_r;
+    }
+}
+
+// Projected / sliced keys.  A wave owns the P = G TW adjacent tokens of its G
+// groups of lanes; each trip forms the dots of four (source, token) pairs of
+// every group.
+template <int FMT, typename T, int LG, int NCH, bool SLICED, CacheGrad OUT, int TW>
+__global__ void __launch_bounds__(kBlock)
+cache_bwd_lr(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
+             const void *__restrict__ K, const float *__restrict__ q, const T *__restrict__ dH,
+             T *__restrict__ dV, T *__restrict__ dK, float *__restrict__ coef,
+             float *__restrict__ partial, int S, int N, int d, int r, float eps, int s_pad,
+             int r_pad)
+{
+    constexpr int G = kWaveSize / LG, CW = unit_cols<FMT>(), P = G * TW, SB = 4 / TW;
+    constexpr int per = kCacheBlock / CW;  // units a block
+    extern __shared__ float lds[];
+    const int lane = threadIdx.x & (kWaveSize - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
+    const int array = kWaves * P * s_pad;  // one of the four: [tokens of the workgroup][s_pad]
+    float *s = lds + wave * P * s_pad, *ri = s + array, *g = ri + array, *alpha = g + array;
+    float *stage = lds + 4 * array;        // [kWaves][r_pad]
+    const int bx = xcd_block().x;
+    const int n0 = (bx * kWaves + wave) * P;
+    const Keys<FMT, T, SLICED> keys(K, codes, scales, N, d, r);
+    const Lanes<FMT, LG, NCH> ln(lane, d);
+    float qk[8], dq_acc[8];
+    keys.query(q, lane % keys.lps, qk);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        dq_acc[e] = 0.0f;
+
+    if (n0 < N) {  // wave-uniform; the barriers are after it
+        float dh[TW][NCH][CW];
+        unsigned at[TW][NCH];
+#pragma unroll
+        for (int t = 0; t < TW; ++t) {
+            const int n = min(n0 + t * G + ln.g, N - 1);
+            load_dh<FMT, T, LG, NCH>(dH + (size_t)n * d, ln, d, dh[t]);
+#pragma unroll
+            for (int c = 0; c < NCH; ++c)
+                at[t][c] = (unsigned)((n - n0) * ln.nu) + ln.at[c];
+        }
+        cache_scores<FMT, T, SLICED, P, P <= 2 ? 4 : P <= 4 ? 2 : 1>(keys, q, 0, S, n0, eps, lane, s,
+                                                                    ri, s_pad);
+        wave_lds_sync();
+#pragma unroll
+        for (int t = 0; t < TW; ++t)
+            group_softmax<LG>(s + t * G * s_pad, alpha + t * G * s_pad, s_pad, S, ln.g, ln.lu);
+
+        // The dots of dH with the stored rows.
+        const size_t first = (size_t)n0 * ln.nu, plane = (size_t)N * ln.nu;
+        for (int i0 = 0; i0 < S; i0 += SB) {
+            UnitRaw<FMT> w[SB][TW][NCH];
+#pragma unroll
+            for (int u = 0; u < SB; ++u) {
+                const size_t b = min(i0 + u, S - 1) * plane + first;
+#pragma unroll
+                for (int t = 0; t < TW; ++t)
+#pragma unroll
+                    for (int c = 0; c < NCH; ++c)
+                        load_unit<FMT>(codes + b * 16, scales + b / per, at[t][c], w[u][t][c]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            float p[4];
+#pragma unroll
+            for (int u = 0; u < SB; ++u)
+#pragma unroll
+                for (int t = 0; t < TW; ++t) {
+                    p[u * TW + t] = 0.0f;
+#pragma unroll
+                    for (int c = 0; c < NCH; ++c)
+                        p[u * TW + t] = dot_unit<FMT>(w[u][t][c], dh[t][c], p[u * TW + t]);
+                }
+            const float sum = four_sums<LG>(p, lane);
+            const int k = four_index<LG>(lane), i = i0 + k / TW;
+            if (lane % (LG / 4) == 0 && i < S)
+                g[(k % TW * G + ln.g) * s_pad + i] = sum;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        wave_lds_sync();
+#pragma unroll
+        for (int t = 0; t < TW; ++t) {
+            float *gr = g + (t * G + ln.g) * s_pad;
+            const float *ar = alpha + (t * G + ln.g) * s_pad;
+            float gb = 0.0f;
+            for (int i = ln.lu; i < S; i += LG)
+                gb = fmaf(ar[i], gr[i], gb);
+            gb = group_sum(gb, LG);
+            for (int i = ln.lu; i < S; i += LG)
+                gr[i] = ar[i] * (gr[i] - gb);  // g now holds ds
+        }
+        wave_lds_sync();
+        for (int t = 0; t < P && n0 + t < N; ++t) {
+            const int o = t * s_pad;
+            key_grads<FMT, T, SLICED, OUT>(keys, dH + (size_t)(n0 + t) * d, dV, dK, qk, 0, S, n0 + t,
+                                           lane, s + o, ri + o, g + o, alpha + o, dq_acc);
+            if constexpr (OUT != kGradCoef)
+                value_grads<T, (NCH * LG * CW + 511) / 512, OUT>(dH + (size_t)(n0 + t) * d, dV, 0, S,
+                                                                n0 + t, N, d,
+                                                                SLICED ? keys.base : d, lane,
+                                                                alpha + o);
+        }
+    }
+    store_dq(keys, dq_acc, stage, r_pad, partial, bx, wave, lane);  // (a barrier: LDS is written)
+    if constexpr (OUT == kGradCoef)
+        store_coef(coef, lds, lds + array, lds + 2 * array, lds + 3 * array, s_pad, kWaves * P,
+                   bx * kWaves * P, 0, S, N, 1.0f / (float)r, threadIdx.x, kBlock);
+}
+
+// The same for few tokens: one token a workgroup, its sources cut into a range a
+// wave, whose groups take every G-th one, U of them in flight a lane; scores and
+// dots of all of them meet in LDS.
+template <int FMT, typename T, int LG, int NCH, bool SLICED, CacheGrad OUT>
+__global__ void __launch_bounds__(kBlock)
+cache_bwd_lr_wg(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
+                const void *__restrict__ K, const float *__restrict__ q, const T *__restrict__ dH,
+                T *__restrict__ dV, T *__restrict__ dK, float *__restrict__ coef,
+                float *__restrict__ partial, int S, int N, int d, int r, float eps, int s_pad,
+                int r_pad)
+{
+    constexpr int G = kWaveSize / LG, CW = unit_cols<FMT>();
+    constexpr int per_block = kCacheBlock / CW, U = NCH >= 4 ? 4 : 8;
+    extern __shared__ float lds[];
+    const int lane = threadIdx.x & (kWaveSize - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
+    float *s = lds, *ri = s + s_pad, *g = ri + s_pad, *ds = g + s_pad;
+    float *alpha = ds + s_pad + wave * s_pad;  // a wave's own
+    float *stage = lds + (4 + kWaves) * s_pad;
+    const int n = xcd_block().x;
+    const int per = (S + kWaves - 1) / kWaves;
+    const int ib = min(S, wave * per), ie = min(S, ib + per);
+    const Keys<FMT, T, SLICED> keys(K, codes, scales, N, d, r);
+    const Lanes<FMT, LG, NCH> ln(lane, d);
+    const T *dhrow = dH + (size_t)n * d;
+    float qk[8], dq_acc[8];
+    keys.query(q, lane % keys.lps, qk);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        dq_acc[e] = 0.0f;
+    if (ib < ie) {  // wave-uniform
+        const size_t first = (size_t)n * ln.nu, plane = (size_t)N * ln.nu;
+        UnitRaw<FMT> w[U][NCH];
+        auto load = [&](int i0) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const size_t b = min(i0 + u * G + ln.g, ie - 1) * plane + first;
+#pragma unroll
+                for (int c = 0; c < NCH; ++c)
+                    load_unit<FMT>(codes + b * 16, scales + b / per_block, ln.at[c], w[u][c]);
+            }
+        };
+        float dh[NCH][CW];
+        load_dh<FMT, T, LG, NCH>(dhrow, ln, d, dh);
+        load(ib);
+        cache_scores<FMT, T, SLICED, 1, 4>(keys, q, ib, ie, n, eps, lane, s, ri, s_pad);
+        for (int i0 = ib; i0 < ie; i0 += U * G) {
+            if (i0 > ib)
+                load(i0);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int h = 0; h < U; h += 4) {
+                float p[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    p[u] = 0.0f;
+#pragma unroll
+                    for (int c = 0; c < NCH; ++c)
+                        p[u] = dot_unit<FMT>(w[h + u][c], dh[c], p[u]);
+                }
+                const float sum = four_sums<LG>(p, lane);
+                const int i = i0 + (h + four_index<LG>(lane)) * G + ln.g;
+                if (lane % (LG / 4) == 0 && i < ie)
+                    g[i] = sum;
+            }
+        }
+    }
+    __syncthreads();
+    float m = -INFINITY, z = 0.0f, gb = 0.0f;
+    for (int i = lane; i < S; i += kWaveSize)
+        m = fmaxf(m, s[i]);
+    m = group_max(m, kWaveSize);
+    for (int i = lane; i < S; i += kWaveSize) {
+        const float e = expf(s[i] - m);
+        alpha[i] = e;
+        z += e;
+    }
+    const float inv = 1.0f / group_sum(z, kWaveSize);
+    for (int i = lane; i < S; i += kWaveSize) {
+        const float a = alpha[i] * inv;
+        alpha[i] = a;
+        gb = fmaf(a, g[i], gb);
+    }
+    gb = group_sum(gb, kWaveSize);
+    wave_lds_sync();
+    for (int i = ib + lane; i < ie; i += kWaveSize)
+        ds[i] = alpha[i] * (g[i] - gb);
+    wave_lds_sync();
+    key_grads<FMT, T, SLICED, OUT>(keys, dhrow, dV, dK, qk, ib, ie, n, lane, s, ri, ds, alpha, dq_acc);
+    if constexpr (OUT == kGradCoef)
+        store_coef(coef, s, ri, ds, alpha, 0, 1, n, ib, ie, N, 1.0f / (float)r, lane, kWaveSize);
+    else
+        value_grads<T, (NCH * LG * CW + 511) / 512, OUT>(dhrow, dV, ib, ie, n, N, d,
+                                                        SLICED ? keys.base : d, lane, alpha);
+    store_dq(keys, dq_acc, stage, r_pad, partial, n, wave, lane);
 }
 
 // Full-rank keys: pass 1 reads the rows for sum(x^2), q.x and dH.x; pass 2 reads
 // them again for dV_i = alpha_i dH + (ds_i / rho_i)(q - x_i s_i / (rho_i d)) and
-// dq.  One token a wave at a time, tpw in turn.
-template <int FMT, typename T, int NCH, bool ADD>
+// dq.  Every group of lanes has a token of its own, tpw in turn.
+template <int FMT, typename T, int LG, int NCH, bool ADD>
 __global__ void __launch_bounds__(kBlock)
 cache_bwd_full(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                const float *__restrict__ q, const T *__restrict__ dH, T *__restrict__ dV,
                float *__restrict__ partial, int S, int N, int d, float eps, int s_pad, int tpw)
 {
+    constexpr int G = kWaveSize / LG, CW = unit_cols<FMT>(), kRow = NCH * LG * CW;
+    constexpr int per = kCacheBlock / CW;  // units a block
     extern __shared__ float lds[];
     const int lane = threadIdx.x & (kWaveSize - 1);
-    const int wave = threadIdx.x / kWaveSize;
-    float *ss = lds + (4 * wave + 0) * s_pad;     // sum x^2, then rho
-    float *sc = lds + (4 * wave + 1) * s_pad;     // q.x, then the score
-    float *g = lds + (4 * wave + 2) * s_pad;      // dH.x, then ds
-    float *alpha = lds + (4 * wave + 3) * s_pad;
-    float *stage = lds + 4 * kWaves * s_pad;      // [NCH * 1024]
-    const int nb = (d + kCacheBlock - 1) / kCacheBlock;
-    const int col = lane * kCacheVec;
-    const bool vec = d % 8 == 0;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
+    const Lanes<FMT, LG, NCH> ln(lane, d);
+    float *sc = lds + (wave * G + ln.g) * 4 * s_pad;  // the group's scores
+    float *ri = sc + s_pad, *g = ri + s_pad, *alpha = g + s_pad;
+    float *stage = lds + kWaves * G * 4 * s_pad;      // [kRow]
     const float inv_d = 1.0f / (float)d;
-    float qv[NCH][16], dqa[NCH][16];
-    bool in[NCH];
+    float qv[NCH][CW], dqa[NCH][CW];
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) {
-        in[c] = col + c * 1024 < nb * kCacheBlock;
+    for (int c = 0; c < NCH; ++c)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int j = col + c * 1024 + e;
+        for (int e = 0; e < CW; ++e) {
+            const int j = ln.col(c) + e;
             qv[c][e] = j < d ? q[j] : 0.0f;
             dqa[c][e] = 0.0f;
         }
-    }
-    const int bx = blockIdx.x;
+    const size_t plane = (size_t)N * ln.nu;
+    const int bx = xcd_block().x;
     for (int t = 0; t < tpw; ++t) {
-        const int n = (bx * tpw + t) * kWaves + wave;
-        if (n >= N)
+        const int n0 = ((bx * tpw + t) * kWaves + wave) * G;
+        if (n0 >= N)
             break;  // wave-uniform; the workgroup barriers are after the loop
-        float dh[NCH][16];
+        const bool live = n0 + ln.g < N;  // a group past the last token adds and writes nothing
+        const int n = min(n0 + ln.g, N - 1);
+        const size_t first = (size_t)n0 * ln.nu;
+        unsigned at[NCH];
+        float dh[NCH][CW];
+        load_dh<FMT, T, LG, NCH>(dH + (size_t)n * d, ln, d, dh);
 #pragma unroll
         for (int c = 0; c < NCH; ++c)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float y[8];
-                load8(dH + (size_t)n * d, col + c * 1024 + 8 * h, d, vec, y);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    dh[c][8 * h + e] = y[e];
-            }
+            at[c] = ln.at[c] + (unsigned)((n - n0) * ln.nu);
         for (int i0 = 0; i0 < S; i0 += 4) {
-            RowRaw<FMT> w[4][NCH];
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int c = 0; c < NCH; ++c)
-                    load_row<FMT>(codes, scales, (size_t)min(i0 + u, S - 1) * N + n, nb,
-                                  RowAt<FMT>(col + c * 1024, nb), w[u][c]);
-            __builtin_amdgcn_sched_barrier(0);
-            float part[16];
+            UnitRaw<FMT> w[4][NCH];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                float a = 0.0f, b = 0.0f, p = 0.0f;
+                const size_t b = min(i0 + u, S - 1) * plane + first;
+#pragma unroll
+                for (int c = 0; c < NCH; ++c)
+                    load_unit<FMT>(codes + b * 16, scales + b / per, at[c], w[u][c]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            float ss[4], dot[4], p[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                ss[u] = dot[u] = p[u] = 0.0f;
 #pragma unroll
                 for (int c = 0; c < NCH; ++c) {
-                    float x[16], ac = 0.0f;
-                    row_values<FMT>(w[u][c], x);
+                    float a = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        ac = fmaf(x[e], x[e], ac);
-                        b = fmaf(qv[c][e], x[e], b);
-                        p = fmaf(dh[c][e], x[e], p);
+                    for (int h = 0; h < CW / 16; ++h) {
+                        float x[16];
+                        unit_values<FMT>(w[u][c], h, x);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            a = fmaf(x[e], x[e], a);
+                            dot[u] = fmaf(qv[c][16 * h + e], x[e], dot[u]);
+                            p[u] = fmaf(dh[c][16 * h + e], x[e], p[u]);
+                        }
                     }
-                    a += in[c] ? ac : 0.0f;
+                    ss[u] += ln.in[c] ? a : 0.0f;
                 }
-                part[u] = a;
-                part[4 + u] = b;
-                part[8 + u] = p;
-                part[12 + u] = 0.0f;
             }
-            const float tot = multi_sum<16>(part, lane);
-            const int idx = multi_sum_index<16>(lane);
-            const int i = i0 + (idx & 3);
-            if (multi_sum_writer<16>(lane) && idx < 12 && i < S)
-                (idx < 4 ? ss : idx < 8 ? sc : g)[i] = tot;
+            const float tss = four_sums<LG>(ss, lane), tdot = four_sums<LG>(dot, lane),
+                        tg = four_sums<LG>(p, lane);
+            const int i = i0 + four_index<LG>(lane);
+            if (lane % (LG / 4) == 0 && i < S) {
+                const float rv = rsqrtf(tss * inv_d + eps);
+                ri[i] = rv;
+                sc[i] = tdot * rv;
+                g[i] = tg;
+            }
         }
         wave_lds_sync();
-        for (int i = lane; i < S; i += kWaveSize) {
-            const float rho = sqrtf(ss[i] / (float)d + eps);
-            ss[i] = rho;
-            sc[i] = sc[i] / rho;
-        }
-        wave_lds_sync();
-        depth_softmax<true>(sc, alpha, S, lane);
+        group_softmax<LG>(sc, alpha, 0, S, 0, ln.lu);
         float gb = 0.0f;
-        for (int i = lane; i < S; i += kWaveSize)
+        for (int i = ln.lu; i < S; i += LG)
             gb = fmaf(alpha[i], g[i], gb);
-        gb = wave_sum_t<true>(gb);
-        for (int i = lane; i < S; i += kWaveSize)
+        gb = group_sum(gb, LG);
+        for (int i = ln.lu; i < S; i += LG)
             g[i] = alpha[i] * (g[i] - gb);
         wave_lds_sync();
 
         for (int i = 0; i < S; ++i) {
             const float a = alpha[i];
-            const float c1 = g[i] / ss[i];                  // ds_i / rho_i
-            const float c2 = c1 * sc[i] / ss[i] * inv_d;    // ds_i s_i / (rho_i^2 d)
+            const float c1 = live ? g[i] * ri[i] : 0.0f;     // ds_i / rho_i
+            const float c2 = c1 * sc[i] * ri[i] * inv_d;     // ds_i s_i / (rho_i^2 d)
             T *orow = dV + ((size_t)i * N + n) * d;
-            RowRaw<FMT> w[NCH];
+            UnitRaw<FMT> w[NCH];
+            const size_t b = i * plane + first;
 #pragma unroll
             for (int c = 0; c < NCH; ++c)
-                load_row<FMT>(codes, scales, (size_t)i * N + n, nb,
-                              RowAt<FMT>(col + c * 1024, nb), w[c]);
+                load_unit<FMT>(codes + b * 16, scales + b / per, at[c], w[c]);
 #pragma unroll
-            for (int c = 0; c < NCH; ++c) {
-                float x[16];
-                row_values<FMT>(w[c], x);
+            for (int c = 0; c < NCH; ++c)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int oc = col + c * 1024 + 8 * h;
-                    float y[8];
+                for (int h = 0; h < CW / 16; ++h) {
+                    float x[16];
+                    unit_values<FMT>(w[c], h, x);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int k = 8 * h + e;
-                        y[e] = fmaf(a, dh[c][k], fmaf(c1, qv[c][k], -c2 * x[k]));
-                        dqa[c][k] = fmaf(c1, x[k], dqa[c][k]);
+                    for (int hh = 0; hh < 2; ++hh) {
+                        const int oc = ln.col(c) + 16 * h + 8 * hh;
+                        float y[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int k = 16 * h + 8 * hh + e;
+                            const float xe = x[8 * hh + e];
+                            y[e] = fmaf(a, dh[c][k], fmaf(c1, qv[c][k], -c2 * xe));
+                            dqa[c][k] = fmaf(c1, xe, dqa[c][k]);
+                        }
+                        if (live) {
+                            if constexpr (ADD) {
+                                float o[8];
+                                load8(orow, oc, d, d % 8 == 0, o);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    y[e] += o[e];
+                            }
+                            store8<T, false>(orow, oc, d, d % 8 == 0, y);
+                        }
                     }
-                    if constexpr (ADD) {
-                        float o[8];
-                        load8(orow, oc, d, vec, o);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            y[e] += o[e];
-                    }
-                    store8<T, false>(orow, oc, d, vec, y);
                 }
-            }
         }
         wave_lds_sync();
     }
-    // dq: the waves add their columns in turn.
-    for (int w = 0; w < kWaves; ++w) {
-        if (wave == w) {
+    // dq: the groups and waves add their columns in turn.
+    for (int w = 0; w < kWaves * G; ++w) {
+        if (wave * G + ln.g == w) {
 #pragma unroll
             for (int c = 0; c < NCH; ++c)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    float *p = stage + c * 1024 + e * 64 + lane;
+                for (int e = 0; e < CW; ++e) {
+                    float *p = stage + (c * CW + e) * LG + ln.lu;
                     *p = (w == 0 ? 0.0f : *p) + dqa[c][e];
                 }
         }
         __syncthreads();
     }
     for (int j = threadIdx.x; j < d; j += kBlock) {
-        const int k = j % 1024;
-        partial[(size_t)bx * d + j] = stage[j - k + k % 16 * 64 + k / 16];
+        const int unit = j / CW, e = j % CW;  // unit = lu + c LG
+        partial[(size_t)bx * d + j] = stage[(unit / LG * CW + e) * LG + unit % LG];
     }
+    static_assert(kRow >= LG, "");
 }
 
 // How a backward is laid out over workgroups.
 struct CacheBwdPlan {
-    bool split;
+    bool split;   // low rank: one token a workgroup
+    bool many;    // low rank: several tokens a group
     int tpw, nblocks;
 };
 CacheBwdPlan cache_bwd_plan(const CacheProblem &p);
+
+// Tokens a group of the low-rank backward where there are many, by chunks.
+constexpr int bwd_many(int nch) { return nch == 1 ? 4 : nch == 2 ? 2 : 1; }
 
 template <int FMT, typename T>
 hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, void *dK,
@@ -415,43 +580,48 @@ hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, 
     const T *dh = static_cast<const T *>(dH);
     T *dv = static_cast<T *>(dV), *dk = static_cast<T *>(dK);
     const int S = (int)p.S, N = (int)p.N, d = (int)p.d, r = (int)p.r;
-    const int s_pad = (S + 3) / 4 * 4, r_pad = (r + 3) / 4 * 4;
-    const size_t slices = (size_t)4 * kWaves * s_pad;
-    return dispatch_row_chunks(p.d, [&](auto nch) -> hipError_t {
-        constexpr int NCH = decltype(nch)::value;
+    const int s_pad = S | 1, r_pad = (r + 3) / 4 * 4;
+    return dispatch_lanes<FMT>(p.d, [&](auto lg, auto nc) -> hipError_t {
+        constexpr int LG = decltype(lg)::value, NCH = decltype(nc)::value, G = kWaveSize / LG;
         if (p.mode == LRAR_MODE_FULL) {
-            const size_t lds = (slices + NCH * 1024) * sizeof(float);
+            const size_t lds = ((size_t)kWaves * G * 4 * s_pad + NCH * LG * unit_cols<FMT>()) * sizeof(float);
             if (accumulate)
-                hipLaunchKernelGGL((cache_bwd_full<FMT, T, NCH, true>), dim3(pl.nblocks),
+                hipLaunchKernelGGL((cache_bwd_full<FMT, T, LG, NCH, true>), dim3(pl.nblocks),
                                    dim3(kBlock), lds, st, p.codes, p.scales, p.q, dh, dv, partial,
                                    S, N, d, p.eps, s_pad, pl.tpw);
             else
-                hipLaunchKernelGGL((cache_bwd_full<FMT, T, NCH, false>), dim3(pl.nblocks),
+                hipLaunchKernelGGL((cache_bwd_full<FMT, T, LG, NCH, false>), dim3(pl.nblocks),
                                    dim3(kBlock), lds, st, p.codes, p.scales, p.q, dh, dv, partial,
                                    S, N, d, p.eps, s_pad, pl.tpw);
             return hipGetLastError();
         }
-        const size_t lds = (slices + kWaves * r_pad) * sizeof(float);
-        auto launch = [&](auto sliced, auto out, auto split) {
-            hipLaunchKernelGGL((cache_bwd_lr<FMT, T, NCH, decltype(sliced)::value,
-                                             decltype(out)::value, decltype(split)::value>),
-                               dim3(pl.nblocks), dim3(kBlock), lds, st, p.codes, p.scales, p.K,
-                               p.q, dh, dv, dk, coef, partial, S, N, d, r, p.eps, s_pad, r_pad,
-                               pl.tpw);
-        };
-        auto by_split = [&](auto sliced, auto out) {
+        auto by_form = [&](auto sliced, auto out) {
+            constexpr bool SL = decltype(sliced)::value;
+            constexpr CacheGrad OUT = decltype(out)::value;
+            auto launch = [&](auto tw) {
+                constexpr int TW = decltype(tw)::value;
+                const size_t lds = ((size_t)4 * kWaves * G * TW * s_pad + kWaves * r_pad) * sizeof(float);
+                hipLaunchKernelGGL((cache_bwd_lr<FMT, T, LG, NCH, SL, OUT, TW>), dim3(pl.nblocks),
+                                   dim3(kBlock), lds, st, p.codes, p.scales, p.K, p.q, dh, dv, dk,
+                                   coef, partial, S, N, d, r, p.eps, s_pad, r_pad);
+            };
             if (pl.split)
-                launch(sliced, out, std::true_type{});
+                hipLaunchKernelGGL((cache_bwd_lr_wg<FMT, T, LG, NCH, SL, OUT>), dim3(pl.nblocks),
+                                   dim3(kBlock), ((4 + kWaves) * s_pad + kWaves * r_pad) * sizeof(float),
+                                   st, p.codes, p.scales, p.K, p.q, dh, dv, dk, coef, partial, S, N,
+                                   d, r, p.eps, s_pad, r_pad);
+            else if (pl.many)
+                launch(std::integral_constant<int, bwd_many(NCH)>{});
             else
-                launch(sliced, out, std::false_type{});
+                launch(std::integral_constant<int, 1>{});
         };
         auto by_out = [&](auto sliced) {
             if (coef)
-                by_split(sliced, std::integral_constant<CacheGrad, kGradCoef>{});
+                by_form(sliced, std::integral_constant<CacheGrad, kGradCoef>{});
             else if (accumulate)
-                by_split(sliced, std::integral_constant<CacheGrad, kGradAdd>{});
+                by_form(sliced, std::integral_constant<CacheGrad, kGradAdd>{});
             else
-                by_split(sliced, std::integral_constant<CacheGrad, kGradWrite>{});
+                by_form(sliced, std::integral_constant<CacheGrad, kGradWrite>{});
         };
         if (p.mode == LRAR_MODE_SLICED)
             by_out(std::true_type{});
@@ -461,7 +631,7 @@ hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, 
     });
 }
 
-// Per format and storage, each in a translation unit of its own.
+// Per format, each in a translation unit of its own.
 hipError_t launch_cache_bwd_fp8(const CacheProblem &p, const void *dH, void *dV, void *dK,
                                 float *coef, float *partial, bool accumulate, hipStream_t st);
 hipError_t launch_cache_bwd_fp4(const CacheProblem &p, const void *dH, void *dV, void *dK,

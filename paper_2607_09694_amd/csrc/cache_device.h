@@ -148,6 +148,48 @@ __device__ __forceinline__ void load8(const T *__restrict__ row, int col, int wi
     }
 }
 
+// The same 8 elements as they are stored.
+template <typename T> struct Raw8 {
+    u32x4_t w[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ void load8_raw(const T *__restrict__ row, int col, int width, bool vec,
+                                          Raw8<T> &x)
+{
+    if (vec) {
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k)
+            x.w[k] = *(reinterpret_cast<const u32x4_t *>(row + col) + k);
+    } else if constexpr (sizeof(T) == 2) {
+        unsigned h[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            h[e] = col + e < width ? row[col + e] : 0u;
+        x.w[0] = u32x4_t{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
+    } else {
+        unsigned h[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            h[e] = col + e < width ? __float_as_uint(row[col + e]) : 0u;
+        x.w[0] = u32x4_t{h[0], h[1], h[2], h[3]};
+        x.w[1] = u32x4_t{h[4], h[5], h[6], h[7]};
+    }
+}
+template <typename T> __device__ __forceinline__ void widen8(const Raw8<T> &r, float (&x)[8])
+{
+    if constexpr (sizeof(T) == 2) {
+        widen(r.w[0], x);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            x[4 * k] = __uint_as_float(r.w[k].x);
+            x[4 * k + 1] = __uint_as_float(r.w[k].y);
+            x[4 * k + 2] = __uint_as_float(r.w[k].z);
+            x[4 * k + 3] = __uint_as_float(r.w[k].w);
+        }
+    }
+}
+
 template <typename T, bool NT>
 __device__ __forceinline__ void store8(T *__restrict__ row, int col, int width, bool vec,
                                        const float (&y)[8])
@@ -170,41 +212,248 @@ __device__ __forceinline__ void store8(T *__restrict__ row, int col, int width, 
 }
 
 // ---------------------------------------------------------------------------
-// Keys: slots of 8 elements, the r key elements from a separate row of K
-// (projected) or the columns [d - r, d) of the cache's row (sliced)
+// Rows: a lane takes 16 bytes of codes at a time (a unit: 16 columns of e4m3, 32
+// of e2m1), LG lanes (16, 32 or 64) a row
 // ---------------------------------------------------------------------------
 
-// How a wave reads the keys of a site.  Sliced keys start at slot column
-// `base` = (d - r) / 8 * 8, of which the first d - r - base elements are not
-// the key's; `lps` lanes (a power of two, at most 64) read one source's key.
+// The codes of a unit and the scale byte of its block.  Rows of LG < 64 lanes
+// share a wave, so that a load instruction covers the adjacent rows of 64 / LG
+// tokens of one source.  (Two loads of 16 bytes a lane, 32 bytes apart from the
+// next lane's, read e4m3 rows 10% to 15% slower.)
+template <int FMT> struct UnitRaw {
+    static constexpr int cols = FMT == LRAR_CACHE_FP8 ? 16 : 32;
+    u32x4_t c;
+    unsigned e;
+};
+template <int FMT> constexpr int unit_cols() { return UnitRaw<FMT>::cols; }
+
+// Unit `at` after the one that codes points to (uniform; scales to its block).
+template <int FMT>
+__device__ __forceinline__ void load_unit(const uint8_t *codes, const uint8_t *scales,
+                                          unsigned at, UnitRaw<FMT> &w)
+{
+    w.c = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(codes + at * 16u));
+    w.e = scales[at * (unsigned)unit_cols<FMT>() / kCacheBlock];
+}
+
+// Columns [16 h, 16 h + 16) of the unit.
+template <int FMT>
+__device__ __forceinline__ void unit_values(const UnitRaw<FMT> &w, int h, float (&x)[16])
+{
+    const float sc = block_scale(w.e);
+    if constexpr (FMT == LRAR_CACHE_FP8) {
+        decode<FMT>(w.c, sc, x);
+    } else {
+        const u32x2_t c = h == 0 ? u32x2_t{w.c.x, w.c.y} : u32x2_t{w.c.z, w.c.w};
+        decode<FMT>(c, sc, x);
+    }
+}
+
+// Lane layout of the rows of d columns: units lu, lu + LG, .. (NCH of them) of the
+// rows of group g.  Lanes past the row re-read its last unit (in range; in[c] says
+// which units count).
+template <int FMT, int LG, int NCH> struct Lanes {
+    static constexpr int groups = kWaveSize / LG;
+    int nu, g, lu;
+    bool in[NCH];
+    unsigned at[NCH];  // unit within the row
+    __device__ Lanes(int lane, int d)
+        : nu((d + kCacheBlock - 1) / kCacheBlock * (kCacheBlock / unit_cols<FMT>())), g(lane / LG),
+          lu(lane % LG)
+    {
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+            in[c] = lu + c * LG < nu;
+            at[c] = (unsigned)min(lu + c * LG, nu - 1);
+        }
+    }
+    __device__ int col(int c) const { return (lu + c * LG) * unit_cols<FMT>(); }
+};
+
+// The units of a row of d columns; calls f(std::integral_constant<int, LG>,
+// std::integral_constant<int, NCH>) with the fewest lanes that hold a row.
+template <int FMT, typename F> hipError_t dispatch_lanes(int64_t d, F &&f)
+{
+    typedef std::integral_constant<int, 64> L64;
+    typedef std::integral_constant<int, 1> One;
+    const int64_t nu = cache_blocks(d) * (kCacheBlock / unit_cols<FMT>());
+    if (nu <= 16)
+        return f(std::integral_constant<int, 16>{}, One{});
+    if (nu <= 32)
+        return f(std::integral_constant<int, 32>{}, One{});
+    if (nu <= 64)
+        return f(L64{}, One{});
+    if constexpr (FMT == LRAR_CACHE_FP8) {
+        if (nu > 128)
+            return f(L64{}, std::integral_constant<int, 4>{});
+    }
+    return f(L64{}, std::integral_constant<int, 2>{});
+}
+
+// Encodes a unit of a row (zeros past its end): e4m3 blocks are two neighbouring
+// lanes', e2m1 blocks one lane's.
+template <int FMT>
+__device__ __forceinline__ void encode_unit(const float (&x)[UnitRaw<FMT>::cols], UnitRaw<FMT> &w)
+{
+    constexpr int CW = unit_cols<FMT>();
+    float top = 0.0f;
+#pragma unroll
+    for (int e = 0; e < CW; ++e)
+        top = max_magnitude(top, x[e]);
+    if constexpr (FMT == LRAR_CACHE_FP8)
+        top = max_magnitude(top, dpp_move<kDppXor1>(top));
+    w.e = scale_byte<FMT>(top);
+    unsigned c[4];
+#pragma unroll
+    for (int h = 0; h < CW / 8; ++h) {
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            y[e] = x[8 * h + e];
+        const typename Codes<FMT>::key_t k = encode<FMT>(y, w.e);
+        if constexpr (FMT == LRAR_CACHE_FP8) {
+            c[2 * h] = k.x;
+            c[2 * h + 1] = k.y;
+        } else {
+            c[h] = k;
+        }
+    }
+    w.c = u32x4_t{c[0], c[1], c[2], c[3]};
+}
+
+template <int FMT>
+__device__ __forceinline__ void store_unit(uint8_t *codes, uint8_t *scales, unsigned at,
+                                           const UnitRaw<FMT> &w)
+{
+    *reinterpret_cast<u32x4_t *>(codes + at * 16u) = w.c;
+    scales[at * (unsigned)unit_cols<FMT>() / kCacheBlock] = (uint8_t)w.e;
+}
+
+// a and b, each summed over the two halves of the wave (or of each pair of rows
+// of 16 lanes): the lower half receives a's sum, the upper half b's.  One gfx950
+// lane swap and one addition.
+__device__ __forceinline__ float halve32(float a, float b)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+__device__ __forceinline__ float halve16(float a, float b)
+{
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+constexpr int kDppRor8 = 0x128;  // row_ror:8, lane i + 8 within each 16
+__device__ __forceinline__ float halve8(float a, float b, int lane)
+{
+    const bool up = (lane & 8) != 0;
+    return (up ? b : a) + dpp_move<kDppRor8>(up ? a : b);
+}
+
+// Four values, each summed over every group of LG lanes: a lane receives the sum
+// of value four_index<LG>(lane) over its own group.
+template <int LG> __device__ __forceinline__ float four_sums(const float (&v)[4], int lane)
+{
+    float a, b, s;
+    if constexpr (LG == 64) {
+        a = halve32(v[0], v[2]);
+        b = halve32(v[1], v[3]);
+        s = halve16(a, b);
+        s += dpp_move<kDppRor8>(s);
+    } else if constexpr (LG == 32) {
+        a = halve16(v[0], v[2]);
+        b = halve16(v[1], v[3]);
+        s = halve8(a, b, lane);
+    } else {
+        a = halve8(v[0], v[2], lane);
+        b = halve8(v[1], v[3], lane);
+        const bool up = (lane & 4) != 0;
+        s = (up ? b : a) + __shfl_xor(up ? a : b, 4, kWaveSize);
+    }
+    if constexpr (LG != 16)
+        s += __shfl_xor(s, 4, kWaveSize);
+    s += dpp_move<kDppXor2>(s);
+    return s + dpp_move<kDppXor1>(s);
+}
+// The lane of the group of `lane` that holds value u.
+template <int LG> __device__ __forceinline__ int four_lane(int lane, int u)
+{
+    constexpr int hi = LG / 2, lo = LG / 4;
+    return (lane & ~(LG - 1)) + (u & 2 ? hi : 0) + (u & 1 ? lo : 0);
+}
+template <int LG> __device__ __forceinline__ int four_index(int lane)
+{
+    constexpr int hi = LG / 2, lo = LG / 4;
+    return (lane & hi ? 2 : 0) + (lane & lo ? 1 : 0);
+}
+// Value u of a lane's group, from the lane that holds it.
+template <int LG> __device__ __forceinline__ float four_value(float s, int lane, int u)
+{
+    if constexpr (LG == 64)
+        return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(s), four_lane<LG>(0, u)));
+    else
+        return __shfl(s, four_lane<LG>(lane, u), kWaveSize);
+}
+
+// Softmax over the S sources of the 64 / LG tokens of a wave, each by its own LG
+// lanes: alpha[g * s_pad + i] from s (which may be alpha itself).  The caller
+// orders the LDS accesses.
+template <int LG>
+__device__ __forceinline__ void group_softmax(const float *s, float *alpha, int s_pad, int S, int g,
+                                              int lu)
+{
+    const float *row = s + g * s_pad;
+    float *out = alpha + g * s_pad;
+    float m = -INFINITY;
+    for (int i = lu; i < S; i += LG)
+        m = fmaxf(m, row[i]);
+    m = group_max(m, LG);
+    float z = 0.0f;
+    for (int i = lu; i < S; i += LG) {
+        const float e = expf(row[i] - m);
+        out[i] = e;
+        z += e;
+    }
+    const float inv = 1.0f / group_sum(z, LG);
+    for (int i = lu; i < S; i += LG)
+        out[i] *= inv;
+}
+
+// ---------------------------------------------------------------------------
+// Keys and scores
+// ---------------------------------------------------------------------------
+
+// How a wave reads keys: slots of 8 elements, of a row of K (projected) or of the
+// columns [d - r, d) of the cache's row (sliced: slots start at column `base` =
+// (d - r) / 8 * 8, whose first `off` elements are not the key's).  `lps` lanes (a
+// power of two, at most 64) read one source's key.
 template <int FMT, typename T, bool SLICED> struct Keys {
     const T *__restrict__ K;
-    const uint8_t *__restrict__ codes, *__restrict__ scales;
-    int N, d, r, nb, base, nkv, lps;
+    const uint8_t *codes, *scales;
+    int N, d, r, nb, base, off, nkv, lps;
     bool vec;
 
     __device__ Keys(const void *K_, const uint8_t *codes_, const uint8_t *scales_, int N_, int d_,
                     int r_)
         : K(static_cast<const T *>(K_)), codes(codes_), scales(scales_), N(N_), d(d_), r(r_),
           nb((d_ + kCacheBlock - 1) / kCacheBlock), base(SLICED ? (d_ - r_) / 8 * 8 : 0),
-          nkv(((SLICED ? d_ - base : r_) + 7) / 8), lps(1), vec(r_ % 8 == 0)
+          off(SLICED ? d_ - r_ - base : 0), nkv((r_ + off + 7) / 8), lps(1), vec(r_ % 8 == 0)
     {
         while (lps < nkv && lps < kWaveSize)
             lps <<= 1;
     }
-    // First of the query's elements that slot v meets (below 0: not the key's).
-    __device__ int first(int v) const { return v * 8 + base - (SLICED ? d - r : 0); }
-    __device__ void query(const float *__restrict__ q, int v, float (&x)[8]) const
+    // First of the key's elements that slot v holds (below 0: not the key's).
+    __device__ int first(int v) const { return v * 8 - off; }
+    __device__ __forceinline__ void query(const float *__restrict__ q, int v, float (&x)[8]) const
     {
         const int j = first(v);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            x[e] = v < nkv && j + e >= 0 && j + e < r ? q[j + e] : 0.0f;
+            x[e] = v < nkv && j + e >= 0 && j + e < r ? q[max(min(j + e, r - 1), 0)] : 0.0f;
     }
     struct Raw {
         typename Codes<FMT>::key_t c;
         unsigned e;
-        float x[8];
+        Raw8<T> p;
     };
     // Slot v of source i and token n (both in range; slots past the key re-read
     // the last one).
@@ -219,38 +468,41 @@ template <int FMT, typename T, bool SLICED> struct Keys {
             w.c = *reinterpret_cast<const typename Codes<FMT>::key_t *>(codes + at);
             w.e = scales[row * nb + (unsigned)col / kCacheBlock];
         } else {
-            load8(K + row * r, v * 8, r, vec, w.x);
+            load8_raw(K + row * r, v * 8, r, vec, w.p);
         }
     }
     // Its values, zeros where the slot's elements are not the key's.
     __device__ __forceinline__ void values(const Raw &w, int v, float (&x)[8]) const
     {
         if constexpr (SLICED) {
-            decode<FMT>(w.c, block_scale(w.e), x);
-            const int j = first(v);
+            decode<FMT>(w.c, block_scale(w.e), x);  // zeros past the row
+            if (off != 0) {                         // uniform
+                const int j = first(v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                x[e] = j + e >= 0 ? x[e] : 0.0f;
+                for (int e = 0; e < 8; ++e)
+                    x[e] = j + e >= 0 ? x[e] : 0.0f;
+            }
         } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                x[e] = w.x[e];
+            widen8(w.p, x);
         }
     }
 };
 
-// Scores s_i = q . k_i / rho_i and (rho_out) rho_i of the sources [ib, ie) of
+// Scores s_i = q . k_i / rho_i and (ri_out) 1 / rho_i of the sources [ib, ie) of
 // TW consecutive tokens (tokens past N are read as token N-1 and not written),
 // into s_out[t * s_pad + i].  A group of lps lanes reads one source's key, so
 // 64 / lps sources are scored together, and KP such groups' loads of every
-// token go out before the first is used.  The caller waits for the LDS writes.
-template <int FMT, typename T, bool SLICED, int TW>
+// token go out before the first is used.  (Slots of 16 bytes, so that fewer lanes
+// read a sliced key, were slower: 11% at 33 sources, 16384 tokens, r = 64, e2m1,
+// the arithmetic being the same and more lanes idle.)  The caller waits for the
+// LDS writes.
+template <int FMT, typename T, bool SLICED, int TW, int KP>
 __device__ __forceinline__ void cache_scores(const Keys<FMT, T, SLICED> &k,
                                              const float *__restrict__ q, int ib, int ie,
                                              int n0, float eps, int lane, float *s_out,
-                                             float *rho_out, int s_pad)
+                                             float *ri_out, int s_pad)
 {
-    constexpr int KP = TW >= 2 ? 2 : 4;
+    typedef Keys<FMT, T, SLICED> Key;
     const int lps = k.lps, spi = kWaveSize / lps;
     const int isub = lane / lps, v = lane % lps;
     const float inv_r = 1.0f / (float)k.r;
@@ -259,20 +511,22 @@ __device__ __forceinline__ void cache_scores(const Keys<FMT, T, SLICED> &k,
         k.query(q, v, qv);
         const bool vok = v < k.nkv;
         for (int i0 = ib; i0 < ie; i0 += KP * spi) {
-            typename Keys<FMT, T, SLICED>::Raw w[TW][KP];
+            typename Key::Raw w[TW][KP];
 #pragma unroll
             for (int t = 0; t < TW; ++t)
 #pragma unroll
                 for (int p = 0; p < KP; ++p)
-                    k.load(min(i0 + p * spi + isub, ie - 1), min(n0 + t, k.N - 1), v, w[t][p]);
+                    if (p == 0 || i0 + p * spi < ie)  // wave-uniform
+                        k.load(min(i0 + p * spi + isub, ie - 1), min(n0 + t, k.N - 1), v, w[t][p]);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < TW; ++t)
 #pragma unroll
                 for (int p = 0; p < KP; ++p) {
-                    float x[8];
+                    if (p > 0 && i0 + p * spi >= ie)
+                        break;
+                    float x[8], ss = 0.0f, dot = 0.0f;
                     k.values(w[t][p], v, x);
-                    float ss = 0.0f, dot = 0.0f;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         ss = fmaf(x[e], x[e], ss);
@@ -283,10 +537,10 @@ __device__ __forceinline__ void cache_scores(const Keys<FMT, T, SLICED> &k,
                     butterfly_sum2<true>(ss, dot, lps);
                     const int i = i0 + p * spi + isub;
                     if (v == 0 && i < ie && n0 + t < k.N) {
-                        const float rho = sqrtf(ss * inv_r + eps);
-                        s_out[t * s_pad + i] = dot / rho;
-                        if (rho_out)
-                            rho_out[t * s_pad + i] = rho;
+                        const float ri = rsqrtf(ss * inv_r + eps);
+                        s_out[t * s_pad + i] = dot * ri;
+                        if (ri_out)
+                            ri_out[t * s_pad + i] = ri;
                     }
                 }
         }
@@ -299,7 +553,7 @@ __device__ __forceinline__ void cache_scores(const Keys<FMT, T, SLICED> &k,
         for (int i = ib; i < ie; ++i) {  // keys of more than 64 slots: the wave reads one
             float ss = 0.0f, dot = 0.0f;
             for (int vv = lane; vv < k.nkv; vv += kWaveSize) {
-                typename Keys<FMT, T, SLICED>::Raw w;
+                typename Key::Raw w;
                 float x[8], qv[8];
                 k.load(i, n, vv, w);
                 k.query(q, vv, qv);
@@ -312,59 +566,13 @@ __device__ __forceinline__ void cache_scores(const Keys<FMT, T, SLICED> &k,
             }
             butterfly_sum2<true>(ss, dot, kWaveSize);
             if (lane == 0) {
-                const float rho = sqrtf(ss * inv_r + eps);
-                s_out[t * s_pad + i] = dot / rho;
-                if (rho_out)
-                    rho_out[t * s_pad + i] = rho;
+                const float ri = rsqrtf(ss * inv_r + eps);
+                s_out[t * s_pad + i] = dot * ri;
+                if (ri_out)
+                    ri_out[t * s_pad + i] = ri;
             }
         }
     }
-}
-
-// Where a lane reads its 16 columns of a chunk of 1024: bytes into the row's
-// codes and the index of its scale.  Lanes past the row re-read its last 16
-// columns (in range; what they compute reaches no output).
-template <int FMT> struct RowAt {
-    int code, scale;
-    __device__ RowAt(int col, int nb)
-    {
-        const int c = min(col, nb * kCacheBlock - kCacheVec);
-        code = c / Codes<FMT>::per_byte;
-        scale = c / kCacheBlock;
-    }
-};
-
-template <int FMT> struct RowRaw {
-    typename Codes<FMT>::row_t c;
-    unsigned e;
-};
-
-template <int FMT>
-__device__ __forceinline__ void load_row(const uint8_t *__restrict__ codes,
-                                         const uint8_t *__restrict__ scales, size_t row, int nb,
-                                         const RowAt<FMT> &at, RowRaw<FMT> &w)
-{
-    typedef typename Codes<FMT>::row_t row_t;
-    const row_t *p = reinterpret_cast<const row_t *>(
-        codes + row * nb * (kCacheBlock / Codes<FMT>::per_byte) + at.code);
-    w.c = __builtin_nontemporal_load(p);
-    w.e = scales[row * nb + at.scale];
-}
-
-template <int FMT>
-__device__ __forceinline__ void row_values(const RowRaw<FMT> &w, float (&x)[16])
-{
-    decode<FMT>(w.c, block_scale(w.e), x);
-}
-
-// Calls f(std::integral_constant<int, NCH>) for rows of up to 1024 NCH columns.
-template <typename F> hipError_t dispatch_row_chunks(int64_t d, F &&f)
-{
-    if (d <= 1024)
-        return f(std::integral_constant<int, 1>{});
-    if (d <= 2048)
-        return f(std::integral_constant<int, 2>{});
-    return f(std::integral_constant<int, 4>{});
 }
 
 }  // namespace lrar

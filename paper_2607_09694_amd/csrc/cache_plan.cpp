@@ -9,9 +9,11 @@ namespace lrar {
 namespace {
 
 // Tokens up to which the low-rank backward splits each token's sources over a
-// workgroup, from this many sources on.
+// workgroup.
 constexpr int64_t kSplitBwd = 512;
-constexpr int64_t kSplitBwdSources = 9;
+// Waves from which a group takes several tokens (two a SIMD), and the sources up
+// to which their statistics fit LDS.
+constexpr int64_t kManyWaves = 2048, kManySources = 128;
 
 }  // namespace
 
@@ -19,19 +21,23 @@ CacheBwdPlan cache_bwd_plan(const CacheProblem &p)
 {
     CacheBwdPlan pl;
     const bool full = p.mode == LRAR_MODE_FULL;
-    pl.split = !full && p.N <= kSplitBwd && p.S >= kSplitBwdSources;
-    pl.tpw = full && p.N >= 4096 ? 4 : 1;
-    const int64_t per = pl.split ? 1 : (int64_t)kWaves * pl.tpw;
+    const int64_t units = cache_blocks(p.d) * (p.format == LRAR_CACHE_FP8 ? 2 : 1);
+    const int64_t groups = units <= 16 ? 4 : units <= 32 ? 2 : 1;  // of lanes in a wave
+    const int many = bwd_many(units <= 64 ? 1 : units <= 128 ? 2 : 4);
+    pl.split = !full && p.N <= kSplitBwd;
+    pl.many = !full && !pl.split && p.S <= kManySources && p.N >= kManyWaves * groups * many;
+    pl.tpw = !full ? 1 : p.N >= 4096 * groups ? 4 : 1;
+    const int64_t per = pl.split ? 1 : kWaves * groups * (pl.many ? many : pl.tpw);
     pl.nblocks = (int)((p.N + per - 1) / per);
     return pl;
 }
 
-// Rows of dq partials.  Of a site of many sources: few may need fewer (their
-// tokens are not split), but a buffer sized for one site of a pass serves all.
+// Rows of dq partials: those of the most sources, which take the fewest tokens a
+// workgroup, so that a buffer sized for one site of a pass serves them all.
 size_t cache_bwd_workspace_bytes(const CacheProblem &p)
 {
     CacheProblem q = p;
-    q.S = std::max(p.S, kSplitBwdSources);
+    q.S = std::max(p.S, kManySources + 1);
     return (size_t)cache_bwd_plan(q).nblocks * (size_t)p.r * sizeof(float);
 }
 
