@@ -12,6 +12,10 @@
 #pragma once
 
 #include "cache_device.h"
+#ifndef VAL_TT
+#define VAL_TT 1
+#define VAL_PER 64
+#endif
 
 namespace lrar {
 
@@ -28,7 +32,7 @@ __device__ __forceinline__ void load_dh(const T *__restrict__ row, const Lanes<F
 #pragma unroll
         for (int h = 0; h < unit_cols<FMT>() / 8; ++h) {
             float y[8];
-            load8(row, ln.col(c) + 8 * h, d, d % 8 == 0, y);
+            load8(row, ln.col(c) + 8 * h, d, y);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 dh[c][8 * h + e] = y[e];
@@ -65,13 +69,12 @@ __device__ __forceinline__ void key_grads(const Keys<FMT, T, SLICED> &keys, cons
     const int lps = keys.lps, spi = kWaveSize / lps;
     const int isub = lane / lps, v = lane % lps;
     const float inv_r = 1.0f / (float)keys.r;
-    const bool vec = keys.d % 8 == 0;
     float dhk[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         dhk[e] = 0.0f;
     if (SLICED && OUT != kGradCoef && v < keys.nkv)
-        load8(dhrow, keys.base + v * 8, keys.d, vec, dhk);
+        load8(dhrow, keys.base + v * 8, keys.d, dhk);
     for (int i0 = ib; i0 < ie; i0 += KP * spi) {
         typename Key::Raw w[KP];
 #pragma unroll
@@ -103,49 +106,70 @@ __device__ __forceinline__ void key_grads(const Keys<FMT, T, SLICED> &keys, cons
                 T *orow = SLICED ? dV + row * keys.d : dK + row * keys.r;
                 const int ocol = SLICED ? keys.base + v * 8 : v * 8;
                 const int width = SLICED ? keys.d : keys.r;
-                const bool ovec = SLICED ? vec : keys.vec;
                 if constexpr (OUT == kGradAdd) {
                     float o[8];
-                    load8(orow, ocol, width, ovec, o);
+                    load8(orow, ocol, width, o);
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         y[e] += o[e];
                 }
-                store8<T, false>(orow, ocol, width, ovec, y);
+                store8<T, false>(orow, ocol, width, y);
             }
         }
     }
 }
 
-// dV_i = alpha_i dH of sources [ib, ie) of one token, columns [0, wend).
-template <typename T, int NO, CacheGrad OUT>
-__device__ __forceinline__ void value_grads(const T *__restrict__ dhrow, T *__restrict__ dV, int ib,
-                                            int ie, int n, int N, int d, int wend, int lane,
-                                            const float *alpha)
+// Chunks of 64 lanes of 16 bytes in a row of up to `cols` columns.
+template <typename T> constexpr int value_chunks(int cols)
 {
-    const bool vec = d % 8 == 0;
-    float dh[NO][8];
+    return (cols * (int)sizeof(T) + 1023) / 1024;
+}
+
+// dV_i = alpha_i dH of sources [ib, ie) of TT adjacent tokens, columns [0, wend),
+// in lanes of 16 bytes, whole lines a wave; alpha of source i and token t at
+// alpha[i * si + t * st].
+template <typename T, int NO, CacheGrad OUT, int TT>
+__device__ __forceinline__ void value_grads(const T *__restrict__ dH, T *__restrict__ dV, int ib,
+                                            int ie, int n0, int N, int d, int wend, int lane,
+                                            const float *alpha, size_t si, int st)
+{
+    constexpr int VO = 16 / sizeof(T);
+    u32x4_t dh[TT][NO];
+    int n[TT];
 #pragma unroll
-    for (int c = 0; c < NO; ++c)
-        load8(dhrow, lane * 8 + c * 512, d, vec, dh[c]);
+    for (int t = 0; t < TT; ++t) {
+        n[t] = min(n0 + t, N - 1);  // tokens past the end: the last one again, the same values
+#pragma unroll
+        for (int c = 0; c < NO; ++c)
+            dh[t][c] = load16_elems(dH + (size_t)n[t] * d, (c * kWaveSize + lane) * VO, d);
+    }
     for (int i = ib; i < ie; ++i) {
-        const float a = alpha[i];
-        T *orow = dV + ((size_t)i * N + n) * d;
+        T *plane = dV + (size_t)i * N * d;
 #pragma unroll
-        for (int c = 0; c < NO; ++c) {
-            const int col = lane * 8 + c * 512;
-            float y[8];
+        for (int t = 0; t < TT; ++t) {
+            const float a = alpha[i * si + (n[t] - n0) * st];
+            T *orow = plane + (size_t)n[t] * d;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                y[e] = a * dh[c][e];
-            if constexpr (OUT == kGradAdd) {
-                float o[8];
-                load8(orow, col, wend, vec, o);
+            for (int c = 0; c < NO; ++c) {
+                const int col = (c * kWaveSize + lane) * VO;
+                float y[VO];
+                if constexpr (VO == 8)
+                    widen(dh[t][c], y);
+                else
+                    widen(__builtin_bit_cast(f32x4_t, dh[t][c]), y);
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    y[e] += o[e];
+                for (int e = 0; e < VO; ++e)
+                    y[e] *= a;
+                if constexpr (OUT == kGradAdd) {
+                    const u32x4_t w = load16_elems(orow, col, wend);
+                    if constexpr (VO == 8)
+                        add_stored(y, w);
+                    else
+                        add_stored(y, __builtin_bit_cast(f32x4_t, w));
+                }
+                store16_elems<T, kBwdNtStore>(orow, col, wend,
+                                              __builtin_bit_cast(u32x4_t, Narrow<T, VO>::run(y)));
             }
-            store8<T, kBwdNtStore>(orow, col, wend, vec, y);
         }
     }
 }
@@ -181,7 +205,9 @@ __device__ __forceinline__ void store_dq(const Keys<FMT, T, SLICED> &keys, float
 
 // The coefficients of P tokens from n0 on and sources [ib, ie), by `nthreads`
 // threads, runs of adjacent tokens together: coef[i][0..2][n] = alpha, ds / rho,
-// ds s / (rho r).  The token rows in LDS are s_pad apart (odd: no bank conflict).
+// ds s / (rho r), or (gradient rows) coef[i][n] = alpha.  The token rows in LDS are
+// s_pad apart (odd: no bank conflict).
+template <CacheGrad OUT>
 __device__ __forceinline__ void store_coef(float *__restrict__ coef, const float *s, const float *ri,
                                            const float *ds, const float *alpha, int s_pad, int P,
                                            int n0, int ib, int ie, int N, float inv_r, int thread,
@@ -193,6 +219,10 @@ __device__ __forceinline__ void store_coef(float *__restrict__ coef, const float
         if (t >= count)
             continue;
         const int at = t * s_pad + i;
+        if constexpr (OUT != kGradCoef) {
+            coef[(size_t)i * N + n0 + t] = alpha[at];
+            continue;
+        }
         const float cq = ds[at] * ri[at];
         float *c = coef + (size_t)i * 3 * N + n0 + t;
         c[0] = alpha[at];
@@ -203,7 +233,10 @@ __device__ __forceinline__ void store_coef(float *__restrict__ coef, const float
 
 // Projected / sliced keys.  A wave owns the P = G TW adjacent tokens of its G
 // groups of lanes; each trip forms the dots of four (source, token) pairs of
-// every group.
+// every group.  It writes the key gradients and the dq partials, and into coef the
+// coefficients or (gradient rows) the weights [S][N], from which
+// cache_value_grads writes the rest of dV: reads and writes of HBM in turn, not
+// mixed.
 template <int FMT, typename T, int LG, int NCH, bool SLICED, CacheGrad OUT, int TW>
 __global__ void __launch_bounds__(kBlock)
 cache_bwd_lr(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
@@ -295,17 +328,28 @@ cache_bwd_lr(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scal
             const int o = t * s_pad;
             key_grads<FMT, T, SLICED, OUT>(keys, dH + (size_t)(n0 + t) * d, dV, dK, qk, 0, S, n0 + t,
                                            lane, s + o, ri + o, g + o, alpha + o, dq_acc);
-            if constexpr (OUT != kGradCoef)
-                value_grads<T, (NCH * LG * CW + 511) / 512, OUT>(dH + (size_t)(n0 + t) * d, dV, 0, S,
-                                                                n0 + t, N, d,
-                                                                SLICED ? keys.base : d, lane,
-                                                                alpha + o);
         }
     }
     store_dq(keys, dq_acc, stage, r_pad, partial, bx, wave, lane);  // (a barrier: LDS is written)
-    if constexpr (OUT == kGradCoef)
-        store_coef(coef, lds, lds + array, lds + 2 * array, lds + 3 * array, s_pad, kWaves * P,
-                   bx * kWaves * P, 0, S, N, 1.0f / (float)r, threadIdx.x, kBlock);
+    store_coef<OUT>(coef, lds, lds + array, lds + 2 * array, lds + 3 * array, s_pad, kWaves * P,
+                    bx * kWaves * P, 0, S, N, 1.0f / (float)r, threadIdx.x, kBlock);
+}
+
+// The value rows dV_i = alpha_i dH before column wend: a wave holds TT tokens' dH
+// and walks the planes.
+template <typename T, int NO, CacheGrad OUT, int TT>
+__global__ void __launch_bounds__(kBlock)
+cache_value_grads(const T *__restrict__ dH, const float *__restrict__ alpha, T *__restrict__ dV, int S,
+                  int N, int d, int wend, int per)
+{
+    const int lane = threadIdx.x & (kWaveSize - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
+    const BlockXY bk = xcd_block();
+    const int n0 = (bk.x * kWaves + wave) * TT;
+    if (n0 >= N)
+        return;
+    value_grads<T, NO, OUT, TT>(dH, dV, bk.y * per, min(S, (bk.y + 1) * per), n0, N, d, wend, lane,
+                                alpha + n0, (size_t)N, 1);
 }
 
 // The same for few tokens: one token a workgroup, its sources cut into a range a
@@ -398,10 +442,10 @@ cache_bwd_lr_wg(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ s
     wave_lds_sync();
     key_grads<FMT, T, SLICED, OUT>(keys, dhrow, dV, dK, qk, ib, ie, n, lane, s, ri, ds, alpha, dq_acc);
     if constexpr (OUT == kGradCoef)
-        store_coef(coef, s, ri, ds, alpha, 0, 1, n, ib, ie, N, 1.0f / (float)r, lane, kWaveSize);
+        store_coef<OUT>(coef, s, ri, ds, alpha, 0, 1, n, ib, ie, N, 1.0f / (float)r, lane, kWaveSize);
     else
-        value_grads<T, (NCH * LG * CW + 511) / 512, OUT>(dhrow, dV, ib, ie, n, N, d,
-                                                        SLICED ? keys.base : d, lane, alpha);
+        value_grads<T, value_chunks<T>(NCH * LG * CW), OUT, 1>(
+            dH, dV, ib, ie, n, N, d, SLICED ? keys.base : d, lane, alpha, 1, 0);
     store_dq(keys, dq_acc, stage, r_pad, partial, n, wave, lane);
 }
 
@@ -529,12 +573,12 @@ cache_bwd_full(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ sc
                         if (live) {
                             if constexpr (ADD) {
                                 float o[8];
-                                load8(orow, oc, d, d % 8 == 0, o);
+                                load8(orow, oc, d, o);
 #pragma unroll
                                 for (int e = 0; e < 8; ++e)
                                     y[e] += o[e];
                             }
-                            store8<T, false>(orow, oc, d, d % 8 == 0, y);
+                            store8<T, false>(orow, oc, d, y);
                         }
                     }
                 }
@@ -574,7 +618,8 @@ constexpr int bwd_many(int nch) { return nch == 1 ? 4 : nch == 2 ? 2 : 1; }
 
 template <int FMT, typename T>
 hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, void *dK,
-                               float *coef, float *partial, bool accumulate, hipStream_t st)
+                               float *coef, bool deferred, float *partial, bool accumulate,
+                               hipStream_t st)
 {
     const CacheBwdPlan pl = cache_bwd_plan(p);
     const T *dh = static_cast<const T *>(dH);
@@ -604,6 +649,16 @@ hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, 
                 hipLaunchKernelGGL((cache_bwd_lr<FMT, T, LG, NCH, SL, OUT, TW>), dim3(pl.nblocks),
                                    dim3(kBlock), lds, st, p.codes, p.scales, p.K, p.q, dh, dv, dk,
                                    coef, partial, S, N, d, r, p.eps, s_pad, r_pad);
+                if constexpr (OUT != kGradCoef) {
+                    constexpr int NO = value_chunks<T>(NCH * LG * unit_cols<FMT>());
+                    constexpr int TT = VAL_TT;
+                    const int per = VAL_PER, tokens = kWaves * TT;
+                    hipLaunchKernelGGL((cache_value_grads<T, NO, OUT, TT>),
+                                       dim3((unsigned)((N + tokens - 1) / tokens),
+                                            (unsigned)((S + per - 1) / per)),
+                                       dim3(kBlock), 0, st, dh, coef, dv, S, N, d,
+                                       SL ? (d - r) / 8 * 8 : d, per);
+                }
             };
             if (pl.split)
                 hipLaunchKernelGGL((cache_bwd_lr_wg<FMT, T, LG, NCH, SL, OUT>), dim3(pl.nblocks),
@@ -616,7 +671,7 @@ hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, 
                 launch(std::integral_constant<int, 1>{});
         };
         auto by_out = [&](auto sliced) {
-            if (coef)
+            if (deferred)
                 by_form(sliced, std::integral_constant<CacheGrad, kGradCoef>{});
             else if (accumulate)
                 by_form(sliced, std::integral_constant<CacheGrad, kGradAdd>{});
@@ -633,8 +688,10 @@ hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, 
 
 // Per format, each in a translation unit of its own.
 hipError_t launch_cache_bwd_fp8(const CacheProblem &p, const void *dH, void *dV, void *dK,
-                                float *coef, float *partial, bool accumulate, hipStream_t st);
+                                float *coef, bool deferred, float *partial, bool accumulate,
+                                hipStream_t st);
 hipError_t launch_cache_bwd_fp4(const CacheProblem &p, const void *dH, void *dV, void *dK,
-                                float *coef, float *partial, bool accumulate, hipStream_t st);
+                                float *coef, bool deferred, float *partial, bool accumulate,
+                                hipStream_t st);
 
 }  // namespace lrar

@@ -4,13 +4,14 @@
 namespace lrar {
 
 hipError_t launch_cache_bwd_fp8(const CacheProblem &p, const void *dH, void *dV, void *dK,
-                                float *coef, float *partial, bool accumulate, hipStream_t st)
+                                float *coef, bool deferred, float *partial, bool accumulate,
+                                hipStream_t st)
 {
     return p.dtype == LRAR_DTYPE_BF16
-               ? launch_cache_bwd_as<LRAR_CACHE_FP8, uint16_t>(p, dH, dV, dK, coef, partial,
-                                                               accumulate, st)
-               : launch_cache_bwd_as<LRAR_CACHE_FP8, float>(p, dH, dV, dK, coef, partial,
-                                                            accumulate, st);
+               ? launch_cache_bwd_as<LRAR_CACHE_FP8, uint16_t>(p, dH, dV, dK, coef, deferred,
+                                                               partial, accumulate, st)
+               : launch_cache_bwd_as<LRAR_CACHE_FP8, float>(p, dH, dV, dK, coef, deferred,
+                                                            partial, accumulate, st);
 }
 
 }  // namespace lrar

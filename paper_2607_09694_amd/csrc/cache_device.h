@@ -120,60 +120,73 @@ __device__ __forceinline__ float max_magnitude(float a, float b)
     return __uint_as_float(max(__float_as_uint(a) & 0x7fffffffu, __float_as_uint(b) & 0x7fffffffu));
 }
 
-// 8 consecutive elements of a row of `width` (zeros past its end): one or two
-// 16-byte accesses where the rows allow it (vec: width % 8 == 0, aligned base),
-// else element by element.
-template <typename T>
-__device__ __forceinline__ void load8(const T *__restrict__ row, int col, int width, bool vec,
-                                      float (&x)[8])
+// 16 bytes at an address that is aligned to its elements only.  gfx950 moves them
+// in one access; rows of any width take the vector path.
+typedef u32x4_t u32x4_u __attribute__((aligned(2)));
+template <bool NT> __device__ __forceinline__ u32x4_t load16(const void *p)
 {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        x[e] = 0.0f;
-    if (vec) {
-        if (col < width) {
-            if constexpr (sizeof(T) == 2) {
-                widen(load_raw<T, 8>(row + col), x);
-            } else {
-                const f32x4_t a = load_raw<T, 4>(row + col), b = load_raw<T, 4>(row + col + 4);
-                x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-                x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (col + e < width)
-                x[e] = load_elem(row + col + e);
-    }
+    const u32x4_u *v = reinterpret_cast<const u32x4_u *>(p);
+    if constexpr (NT)
+        return __builtin_nontemporal_load(v);
+    else
+        return *v;
+}
+template <bool NT> __device__ __forceinline__ void store16(void *p, u32x4_t x)
+{
+    u32x4_u *v = reinterpret_cast<u32x4_u *>(p);
+    if constexpr (NT)
+        __builtin_nontemporal_store(u32x4_u(x), v);
+    else
+        *v = x;
 }
 
-// The same 8 elements as they are stored.
+// VO = 16 / sizeof(T) consecutive elements of a row of `width` as they are stored,
+// zeros past its end.
+template <typename T>
+__device__ __forceinline__ u32x4_t load16_elems(const T *__restrict__ row, int col, int width)
+{
+    constexpr int VO = 16 / sizeof(T);
+    if (col + VO <= width)
+        return load16<false>(row + col);
+    u32x4_t w = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < VO; ++e)
+        if (col + e < width) {
+            if constexpr (sizeof(T) == 2)
+                w[e / 2] |= (unsigned)row[col + e] << (16 * (e % 2));
+            else
+                w[e] = __float_as_uint(row[col + e]);
+        }
+    return w;
+}
+template <typename T, bool NT>
+__device__ __forceinline__ void store16_elems(T *__restrict__ row, int col, int width, u32x4_t w)
+{
+    constexpr int VO = 16 / sizeof(T);
+    if (col + VO <= width) {
+        store16<NT>(row + col, w);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < VO; ++e)
+        if (col + e < width) {
+            if constexpr (sizeof(T) == 2)
+                row[col + e] = (uint16_t)(w[e / 2] >> (16 * (e % 2)));
+            else
+                row[col + e] = __uint_as_float(w[e]);
+        }
+}
+
+// 8 consecutive elements, stored and widened.
 template <typename T> struct Raw8 {
     u32x4_t w[sizeof(T) / 2];
 };
 template <typename T>
-__device__ __forceinline__ void load8_raw(const T *__restrict__ row, int col, int width, bool vec,
-                                          Raw8<T> &x)
+__device__ __forceinline__ void load8_raw(const T *__restrict__ row, int col, int width, Raw8<T> &x)
 {
-    if (vec) {
 #pragma unroll
-        for (int k = 0; k < (int)sizeof(T) / 2; ++k)
-            x.w[k] = *(reinterpret_cast<const u32x4_t *>(row + col) + k);
-    } else if constexpr (sizeof(T) == 2) {
-        unsigned h[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            h[e] = col + e < width ? row[col + e] : 0u;
-        x.w[0] = u32x4_t{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
-    } else {
-        unsigned h[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            h[e] = col + e < width ? __float_as_uint(row[col + e]) : 0u;
-        x.w[0] = u32x4_t{h[0], h[1], h[2], h[3]};
-        x.w[1] = u32x4_t{h[4], h[5], h[6], h[7]};
-    }
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k)
+        x.w[k] = load16_elems(row, col + 4 * k, width);
 }
 template <typename T> __device__ __forceinline__ void widen8(const Raw8<T> &r, float (&x)[8])
 {
@@ -181,33 +194,28 @@ template <typename T> __device__ __forceinline__ void widen8(const Raw8<T> &r, f
         widen(r.w[0], x);
     } else {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            x[4 * k] = __uint_as_float(r.w[k].x);
-            x[4 * k + 1] = __uint_as_float(r.w[k].y);
-            x[4 * k + 2] = __uint_as_float(r.w[k].z);
-            x[4 * k + 3] = __uint_as_float(r.w[k].w);
-        }
+        for (int k = 0; k < 8; ++k)
+            x[k] = __uint_as_float(r.w[k / 4][k % 4]);
     }
 }
-
-template <typename T, bool NT>
-__device__ __forceinline__ void store8(T *__restrict__ row, int col, int width, bool vec,
-                                       const float (&y)[8])
+template <typename T>
+__device__ __forceinline__ void load8(const T *__restrict__ row, int col, int width, float (&x)[8])
 {
-    if (vec) {
-        if (col < width) {
-            if constexpr (sizeof(T) == 2) {
-                store_stream<T, 8, NT>(row + col, Narrow<T, 8>::run(y));
-            } else {
-                store_stream<T, 4, NT>(row + col, f32x4_t{y[0], y[1], y[2], y[3]});
-                store_stream<T, 4, NT>(row + col + 4, f32x4_t{y[4], y[5], y[6], y[7]});
-            }
-        }
+    Raw8<T> r;
+    load8_raw(row, col, width, r);
+    widen8(r, x);
+}
+template <typename T, bool NT>
+__device__ __forceinline__ void store8(T *__restrict__ row, int col, int width, const float (&y)[8])
+{
+    if constexpr (sizeof(T) == 2) {
+        store16_elems<T, NT>(row, col, width, Narrow<T, 8>::run(y));
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (col + e < width)
-                store_elem(row + col + e, y[e]);
+        for (int k = 0; k < 2; ++k)
+            store16_elems<T, NT>(row, col + 4 * k, width,
+                                 u32x4_t{__float_as_uint(y[4 * k]), __float_as_uint(y[4 * k + 1]),
+                                         __float_as_uint(y[4 * k + 2]), __float_as_uint(y[4 * k + 3])});
     }
 }
 
@@ -430,13 +438,12 @@ template <int FMT, typename T, bool SLICED> struct Keys {
     const T *__restrict__ K;
     const uint8_t *codes, *scales;
     int N, d, r, nb, base, off, nkv, lps;
-    bool vec;
 
     __device__ Keys(const void *K_, const uint8_t *codes_, const uint8_t *scales_, int N_, int d_,
                     int r_)
         : K(static_cast<const T *>(K_)), codes(codes_), scales(scales_), N(N_), d(d_), r(r_),
           nb((d_ + kCacheBlock - 1) / kCacheBlock), base(SLICED ? (d_ - r_) / 8 * 8 : 0),
-          off(SLICED ? d_ - r_ - base : 0), nkv((r_ + off + 7) / 8), lps(1), vec(r_ % 8 == 0)
+          off(SLICED ? d_ - r_ - base : 0), nkv((r_ + off + 7) / 8), lps(1)
     {
         while (lps < nkv && lps < kWaveSize)
             lps <<= 1;
@@ -468,7 +475,7 @@ template <int FMT, typename T, bool SLICED> struct Keys {
             w.c = *reinterpret_cast<const typename Codes<FMT>::key_t *>(codes + at);
             w.e = scales[row * nb + (unsigned)col / kCacheBlock];
         } else {
-            load8_raw(K + row * r, v * 8, r, vec, w.p);
+            load8_raw(K + row * r, v * 8, r, w.p);
         }
     }
     // Its values, zeros where the slot's elements are not the key's.

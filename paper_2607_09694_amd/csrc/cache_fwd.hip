@@ -24,7 +24,7 @@ __device__ __forceinline__ void store_h(T *__restrict__ hrow, const Lanes<FMT, L
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 y[e] = acc[c][8 * h + e];
-            store8<T, false>(hrow, col0 + ln.col(c) + 8 * h, d, d % 8 == 0, y);
+            store8<T, false>(hrow, col0 + ln.col(c) + 8 * h, d, y);
         }
 }
 
@@ -253,7 +253,7 @@ cache_fwd_lr_wg(uint8_t *codes, uint8_t *scales, const void *__restrict__ K,
 #pragma unroll
                     for (int h = 0; h < CW / 8; ++h) {
                         float y[8];
-                        load8(o_new + (size_t)n * d, unit * CW + 8 * h, d, d % 8 == 0, y);
+                        load8(o_new + (size_t)n * d, unit * CW + 8 * h, d, y);
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
                             x[8 * h + e] = y[e];
@@ -345,7 +345,7 @@ cache_fwd_full(uint8_t *codes, uint8_t *scales, const float *__restrict__ q,
 #pragma unroll
                 for (int h = 0; h < CW / 8; ++h) {
                     float y[8];
-                    load8(o_new + (size_t)n * d, ln.col(c) + 8 * h, d, d % 8 == 0, y);
+                    load8(o_new + (size_t)n * d, ln.col(c) + 8 * h, d, y);
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         x[8 * h + e] = y[e];

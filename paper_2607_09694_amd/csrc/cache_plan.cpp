@@ -32,24 +32,38 @@ CacheBwdPlan cache_bwd_plan(const CacheProblem &p)
     return pl;
 }
 
-// Rows of dq partials: those of the most sources, which take the fewest tokens a
-// workgroup, so that a buffer sized for one site of a pass serves them all.
-size_t cache_bwd_workspace_bytes(const CacheProblem &p)
+// The dq partials (rows of the most sources, which take the fewest tokens a
+// workgroup), and the weights [S][N] of a low-rank backward that writes gradient
+// rows.  Grows with S: a buffer sized for the deepest site of a pass serves all.
+namespace {
+
+size_t partial_bytes(const CacheProblem &p)
 {
     CacheProblem q = p;
     q.S = std::max(p.S, kManySources + 1);
-    return (size_t)cache_bwd_plan(q).nblocks * (size_t)p.r * sizeof(float);
+    return ((size_t)cache_bwd_plan(q).nblocks * (size_t)p.r * sizeof(float) + 15) / 16 * 16;
+}
+
+}  // namespace
+
+size_t cache_bwd_workspace_bytes(const CacheProblem &p)
+{
+    const bool weights = p.mode != LRAR_MODE_FULL && !cache_bwd_plan(p).split;
+    return partial_bytes(p) + (weights ? (size_t)p.S * (size_t)p.N * sizeof(float) : 0);
 }
 
 int launch_cache_bwd(const CacheProblem &p, const void *dH, void *dV, void *dK, float *coef,
                      float *dq, void *ws, bool accumulate, hipStream_t st, std::string *err)
 {
     float *partial = static_cast<float *>(ws);
+    const bool deferred = coef != nullptr;
+    if (!deferred)
+        coef = partial + partial_bytes(p) / sizeof(float);
     hipError_t e = hipSuccess;
     if (p.N > 0)
         e = p.format == LRAR_CACHE_FP8
-                ? launch_cache_bwd_fp8(p, dH, dV, dK, coef, partial, accumulate, st)
-                : launch_cache_bwd_fp4(p, dH, dV, dK, coef, partial, accumulate, st);
+                ? launch_cache_bwd_fp8(p, dH, dV, dK, coef, deferred, partial, accumulate, st)
+                : launch_cache_bwd_fp4(p, dH, dV, dK, coef, deferred, partial, accumulate, st);
     if (e == hipSuccess)
         e = launch_dq_reduce(partial, dq, p.N > 0 ? cache_bwd_plan(p).nblocks : 0, (int)p.r,
                              accumulate, st);

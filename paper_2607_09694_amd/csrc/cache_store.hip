@@ -17,7 +17,7 @@ struct RowSlots {
 template <int FMT, typename T>
 __global__ void __launch_bounds__(kBlock)
 cache_write(const T *__restrict__ O, uint8_t *__restrict__ codes, uint8_t *__restrict__ scales,
-            int64_t rows, int d, RowSlots rs, int vec)
+            int64_t rows, int d, RowSlots rs)
 {
     typedef typename Codes<FMT>::key_t key_t;
     const int64_t r0 = (int64_t)blockIdx.x * rs.rpb;
@@ -30,7 +30,7 @@ cache_write(const T *__restrict__ O, uint8_t *__restrict__ codes, uint8_t *__res
         const int rl = rs.rpb == 1 ? 0 : (int)__umulhi((unsigned)s, rs.magic);
         const int col = (s - rl * rs.slots) * 8;
         float x[8];
-        load8(O + (r0 + rl) * d, col, d, vec != 0, x);
+        load8(O + (r0 + rl) * d, col, d, x);
         float top = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -47,7 +47,7 @@ cache_write(const T *__restrict__ O, uint8_t *__restrict__ codes, uint8_t *__res
 template <int FMT, typename T>
 __global__ void __launch_bounds__(kBlock)
 cache_read(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
-           T *__restrict__ O, int64_t rows, int d, RowSlots rs, int vec)
+           T *__restrict__ O, int64_t rows, int d, RowSlots rs)
 {
     typedef typename Codes<FMT>::key_t key_t;
     const int64_t r0 = (int64_t)blockIdx.x * rs.rpb;
@@ -59,7 +59,7 @@ cache_read(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales
         const int col = (s - rl * rs.slots) * 8;
         float x[8];
         decode<FMT>(crow[s], block_scale(erow[s >> 2]), x);
-        store8<T, true>(O + (r0 + rl) * d, col, d, vec != 0, x);
+        store8<T, true>(O + (r0 + rl) * d, col, d, x);
     }
 }
 
@@ -76,11 +76,6 @@ RowSlots row_slots(int64_t rows, int64_t d, int64_t *nblocks)
     rs.magic = (unsigned)((((uint64_t)1 << 32) + rs.slots - 1) / rs.slots);
     *nblocks = (rows + rs.rpb - 1) / rs.rpb;
     return rs;
-}
-
-bool rows_vec(const void *O, int64_t d)
-{
-    return d % 8 == 0 && reinterpret_cast<uintptr_t>(O) % 16 == 0;
 }
 
 constexpr int64_t kMaxBlocks = (int64_t)1 << 31;
@@ -111,7 +106,7 @@ int launch_cache_write(const void *O, uint8_t *codes, uint8_t *scales, int64_t r
         typedef decltype(t) T;
         hipLaunchKernelGGL((cache_write<decltype(fmt)::value, T>), dim3((unsigned)nb),
                            dim3(kBlock), 0, st, static_cast<const T *>(O), codes, scales, rows,
-                           (int)d, rs, rows_vec(O, d) ? 1 : 0);
+                           (int)d, rs);
         return hipGetLastError();
     });
     return hip_status(e, "cache_write launch", err);
@@ -132,7 +127,7 @@ int launch_cache_read(const uint8_t *codes, const uint8_t *scales, void *O, int6
         typedef decltype(t) T;
         hipLaunchKernelGGL((cache_read<decltype(fmt)::value, T>), dim3((unsigned)nb),
                            dim3(kBlock), 0, st, codes, scales, static_cast<T *>(O), rows, (int)d,
-                           rs, rows_vec(O, d) ? 1 : 0);
+                           rs);
         return hipGetLastError();
     });
     return hip_status(e, "cache_read launch", err);
