@@ -85,7 +85,7 @@ int lr_attnres_cache_route_fwd(void *codes, void *scales, const void *K, const f
  *   dH [N][d], dV [S][N][d], dK [S][N][r] (projected keys, else NULL) storage
  *   `dtype`, dq [r] fp32; accumulate = 0 overwrites dV, dK and dq, 1 adds.
  *   workspace: lr_attnres_cache_route_bwd_workspace_bytes(...) bytes, 16-byte
- *   aligned (NULL when that is 0), the same for every number of sources.
+ *   aligned (NULL when that is 0); what serves S sources serves fewer.
  * Results are bitwise reproducible.  Errors as for lr_attnres_route_bwd, plus
  * EINVAL for an unknown format and accumulate not 0 or 1.  EUNSUPPORTED:
  * S > 512, N > 2^30, projected or sliced keys with r > 256, d > 4096.

@@ -838,48 +838,60 @@ def source_cache(S: int, N: int, d: int, fmt="fp8", device="cuda") -> SourceCach
                        torch.ones((S, N, nb), dtype=torch.uint8, device=device), d, f)
 
 
-def _cache_args(cache):
-    return _dev(cache.codes, "codes"), _dev(cache.scales, "scales")
+def _on(t, name, index, dtype=None):
+    """t's address, if it is contiguous and on device `index` (None for None)."""
+    if t is None:
+        return None
+    if t.get_device() != index or index < 0:
+        raise ValueError(f"{name} must be a device tensor" if not t.is_cuda else
+                         f"all tensors must be on one device, {name} is on {t.device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    return t.data_ptr()
 
 
-def _cache_site(cache, K, q, mode, others):
-    """Shapes and devices of one read site over a cache; (S, N, d, r)."""
+def _cache_site(cache, K, q, mode):
+    """Shapes of one read site over a cache: (S, N, d, r)."""
     S, N, d = cache._shape
     if mode == PROJECTED:
         if K is None or K.dim() != 3 or K.shape[0] != S or K.shape[1] != N:
             raise ValueError("K must be [S, N, r] for projected keys")
+        r = K.shape[2]
     elif K is not None:
         raise ValueError("K must be None unless keys are projected")
-    r = K.shape[2] if mode == PROJECTED else q.shape[0]
+    else:
+        r = q.shape[0]
     if q.dim() != 1 or q.shape[0] != r:
         raise ValueError(f"q must have shape ({r},)")
-    _same_device(cache.codes, cache.scales, K, q, *others)
     return S, N, d, r
 
 
-def _same_device(first, *others):
-    dev = first.device
-    for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError(f"all tensors must be on {dev}, got one on {t.device}")
-
-
 def _shaped(t, shape, name):
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
-    return t
 
 
-def _call(lib, fn, t, *args):
-    """fn(*args, stream) on t's device, whichever is current."""
+def _cache_call(lib, fn, index, *args):
+    """fn(*args, stream) on device `index`, whichever is current."""
     import torch
 
-    index = t.get_device()
-    if index == torch.cuda.current_device():
-        _check(lib, fn(*args, _stream(t)))
+    if index == torch._C._cuda_getDevice():
+        rc = fn(*args, _raw_stream_of(index))
     else:
         with torch.cuda.device(index):
-            _check(lib, fn(*args, _stream(t)))
+            rc = fn(*args, _raw_stream_of(index))
+    if rc != 0:
+        _check(lib, rc)
+
+
+def _raw_stream_of(index):
+    """The current stream of device `index`, as its handle."""
+    import torch
+
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw else torch.cuda.current_stream(index).cuda_stream
 
 
 def cache_write(cache, O):
@@ -888,12 +900,11 @@ def cache_write(cache, O):
     columns the power of two is the smallest for which nothing saturates; codes
     round to nearest even; a block with a NaN or an infinity reads as NaN."""
     lib = load_library()
+    _shaped(O, cache._shape, "O")
     S, N, d = cache._shape
-    _shaped(O, (S, N, d), "O")
-    _same_device(cache.codes, cache.scales, O)
-    codes, scales = _cache_args(cache)
-    _call(lib, lib.lr_attnres_cache_write, cache.codes, _dev(O, "O"), codes, scales, S * N, d,
-          cache.fmt, _dtype_code(O))
+    dev = cache.codes.get_device()
+    _cache_call(lib, lib.lr_attnres_cache_write, dev, _on(O, "O", dev), _on(cache.codes, "codes", dev),
+                _on(cache.scales, "scales", dev), S * N, d, cache.fmt, _dtype_code(O))
 
 
 def cache_read(cache, dtype=None, out=None):
@@ -904,14 +915,15 @@ def cache_read(cache, dtype=None, out=None):
     lib = load_library()
     if out is None:
         out = torch.empty(cache._shape, dtype=dtype or torch.bfloat16, device=cache.codes.device)
-    elif dtype is not None and out.dtype != dtype:
-        raise TypeError(f"out must be {dtype}, got {out.dtype}")
+    else:
+        if dtype is not None and out.dtype != dtype:
+            raise TypeError(f"out must be {dtype}, got {out.dtype}")
+        _shaped(out, cache._shape, "out")
     S, N, d = cache._shape
-    _shaped(out, (S, N, d), "out")
-    _same_device(cache.codes, cache.scales, out)
-    codes, scales = _cache_args(cache)
-    _call(lib, lib.lr_attnres_cache_read, cache.codes, codes, scales, _dev(out, "out"), S * N, d,
-          cache.fmt, _dtype_code(out))
+    dev = cache.codes.get_device()
+    _cache_call(lib, lib.lr_attnres_cache_read, dev, _on(cache.codes, "codes", dev),
+                _on(cache.scales, "scales", dev), _on(out, "out", dev), S * N, d, cache.fmt,
+                _dtype_code(out))
     return out
 
 
@@ -929,22 +941,26 @@ def cache_route_fwd(cache, K, q, mode, eps: float = 1e-6, o_new=None, dtype=None
 
     lib = load_library()
     mode = _mode(mode)
-    S, N, d, r = _cache_site(cache, K, q, mode, (o_new, out))
+    S, N, d, r = _cache_site(cache, K, q, mode)
     if dtype is None:
         dtype = next((t.dtype for t in (out, K, o_new) if t is not None), torch.bfloat16)
-    H = _shaped(out, (N, d), "out") if out is not None else torch.empty((N, d), dtype=dtype,
-                                                                      device=q.device)
+    if out is None:
+        out = torch.empty((N, d), dtype=dtype, device=q.device)
+    else:
+        _shaped(out, (N, d), "out")
     if o_new is not None:
         _shaped(o_new, (N, d), "o_new")
-    codes, scales = _cache_args(cache)
-    _call(lib, lib.lr_attnres_cache_route_fwd, cache.codes, codes, scales, _dev(K, "K", dtype),
-          _dev(q, "q", torch.float32), _dev(o_new, "o_new", dtype), _dev(H, "H", dtype), S, N, d,
-          r, mode, cache.fmt, _dtype_code(H), float(eps))
-    return H
+    dev = cache.codes.get_device()
+    _cache_call(lib, lib.lr_attnres_cache_route_fwd, dev, _on(cache.codes, "codes", dev),
+                _on(cache.scales, "scales", dev), _on(K, "K", dev, dtype),
+                _on(q, "q", dev, torch.float32), _on(o_new, "o_new", dev, dtype),
+                _on(out, "out", dev, dtype), S, N, d, r, mode, cache.fmt, _dtype_code(out), float(eps))
+    return out
 
 
 def cache_route_bwd_workspace_bytes(S, N, d, r, mode, fmt, dtype) -> int:
-    """Workspace bytes of cache_route_bwd and cache_route_bwd_deferred."""
+    """Workspace bytes of cache_route_bwd and cache_route_bwd_deferred for up to S
+    sources."""
     import torch
 
     code = _BF16 if dtype == torch.bfloat16 else _F32
@@ -953,12 +969,9 @@ def cache_route_bwd_workspace_bytes(S, N, d, r, mode, fmt, dtype) -> int:
                                                                      code)
 
 
-def _cache_workspace(lib, workspace, dH, S, N, d, r, mode, fmt, code):
+def _cache_workspace(lib, dH, S, N, d, r, mode, fmt, code):
     import torch
 
-    if workspace is not None:
-        _same_device(dH, workspace)
-        return workspace
     need = lib.lr_attnres_cache_route_bwd_workspace_bytes(S, N, d, r, mode, fmt, code)
     return torch.empty((max(need, 16),), dtype=torch.uint8, device=dH.device)
 
@@ -978,16 +991,16 @@ def cache_route_bwd(cache, K, q, dH, mode, eps: float = 1e-6, out=None, workspac
 
     lib = load_library()
     mode = _mode(mode)
-    dV, dK, dq = out if out is not None else (None, None, None)
-    S, N, d, r = _cache_site(cache, K, q, mode, (dH, dV, dK, dq))
+    S, N, d, r = _cache_site(cache, K, q, mode)
     _shaped(dH, (N, d), "dH")
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the out=(dV, dK, dq) buffers to add into")
-        dV = torch.empty((S, N, d), dtype=dH.dtype, device=dH.device)
+        dV = dH.new_empty((S, N, d))
         dK = torch.empty_like(K) if mode == PROJECTED else None
-        dq = torch.empty((r,), dtype=torch.float32, device=dH.device)
+        dq = torch.empty_like(q)
     else:
+        dV, dK, dq = out
         _shaped(dV, (S, N, d), "dV")
         _shaped(dq, (r,), "dq")
         if (dK is not None) != (mode == PROJECTED):
@@ -995,13 +1008,15 @@ def cache_route_bwd(cache, K, q, dH, mode, eps: float = 1e-6, out=None, workspac
         if dK is not None:
             _shaped(dK, (S, N, r), "dK")
     code, dt = _dtype_code(dH), dH.dtype
-    workspace = _cache_workspace(lib, workspace, dH, S, N, d, r, mode, cache.fmt, code)
-    codes, scales = _cache_args(cache)
-    _call(lib, lib.lr_attnres_cache_route_bwd, dH, codes, scales, _dev(K, "K", dt),
-          _dev(q, "q", torch.float32), _dev(dH, "dH"), _dev(dV, "dV", dt), _dev(dK, "dK", dt),
-          _dev(dq, "dq", torch.float32), _dev(workspace, "workspace"),
-          workspace.numel() * workspace.element_size(), S, N, d, r, mode, cache.fmt, code,
-          float(eps), int(bool(accumulate)))
+    if workspace is None:
+        workspace = _cache_workspace(lib, dH, S, N, d, r, mode, cache.fmt, code)
+    dev = cache.codes.get_device()
+    _cache_call(lib, lib.lr_attnres_cache_route_bwd, dev, _on(cache.codes, "codes", dev),
+                _on(cache.scales, "scales", dev), _on(K, "K", dev, dt),
+                _on(q, "q", dev, torch.float32), _on(dH, "dH", dev), _on(dV, "dV", dev, dt),
+                _on(dK, "dK", dev, dt), _on(dq, "dq", dev, torch.float32),
+                _on(workspace, "workspace", dev), workspace.numel() * workspace.element_size(), S, N,
+                d, r, mode, cache.fmt, code, float(eps), int(bool(accumulate)))
     return dV, dK, dq
 
 
@@ -1016,19 +1031,21 @@ def cache_route_bwd_deferred(cache, K, q, dH, mode, coef, eps: float = 1e-6, dq=
 
     lib = load_library()
     mode = _mode(mode)
-    S, N, d, r = _cache_site(cache, K, q, mode, (dH, coef, dq))
+    S, N, d, r = _cache_site(cache, K, q, mode)
     _shaped(dH, (N, d), "dH")
     _shaped(coef, (S, 3, N), "coef")
     if dq is None:
-        dq = torch.empty((r,), dtype=torch.float32, device=dH.device)
+        dq = torch.empty_like(q)
     else:
         _shaped(dq, (r,), "dq")
     code = _dtype_code(dH)
-    workspace = _cache_workspace(lib, workspace, dH, S, N, d, r, mode, cache.fmt, code)
-    codes, scales = _cache_args(cache)
-    _call(lib, lib.lr_attnres_cache_route_bwd_deferred, dH, codes, scales,
-          _dev(K, "K", dH.dtype), _dev(q, "q", torch.float32), _dev(dH, "dH"),
-          _dev(coef, "coef", torch.float32), _dev(dq, "dq", torch.float32),
-          _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(), S, N, d, r,
-          mode, cache.fmt, code, float(eps))
+    if workspace is None:
+        workspace = _cache_workspace(lib, dH, S, N, d, r, mode, cache.fmt, code)
+    dev = cache.codes.get_device()
+    _cache_call(lib, lib.lr_attnres_cache_route_bwd_deferred, dev, _on(cache.codes, "codes", dev),
+                _on(cache.scales, "scales", dev), _on(K, "K", dev, dH.dtype),
+                _on(q, "q", dev, torch.float32), _on(dH, "dH", dev),
+                _on(coef, "coef", dev, torch.float32), _on(dq, "dq", dev, torch.float32),
+                _on(workspace, "workspace", dev), workspace.numel() * workspace.element_size(), S, N,
+                d, r, mode, cache.fmt, code, float(eps))
     return dq

@@ -12,10 +12,6 @@
 #pragma once
 
 #include "cache_device.h"
-#ifndef VAL_TT
-#define VAL_TT 1
-#define VAL_PER 64
-#endif
 
 namespace lrar {
 
@@ -176,7 +172,7 @@ __device__ __forceinline__ void value_grads(const T *__restrict__ dH, T *__restr
 
 // The workgroup's dq: over the source groups of each wave (lanes of the same
 // key slot), then over the waves in order, into partial[bx][r].
-template <int FMT, typename T, bool SLICED>
+template <int W, int FMT, typename T, bool SLICED>
 __device__ __forceinline__ void store_dq(const Keys<FMT, T, SLICED> &keys, float (&dq_acc)[8],
                                          float *stage, int r_pad, float *__restrict__ partial, int bx,
                                          int wave, int lane)
@@ -195,9 +191,9 @@ __device__ __forceinline__ void store_dq(const Keys<FMT, T, SLICED> &keys, float
                 my[j + e] = dq_acc[e];
     }
     __syncthreads();
-    for (int j = threadIdx.x; j < r; j += kBlock) {
+    for (int j = threadIdx.x; j < r; j += W * kWaveSize) {
         float sum = 0.0f;
-        for (int w = 0; w < kWaves; ++w)
+        for (int w = 0; w < W; ++w)
             sum += stage[w * r_pad + j];
         partial[(size_t)bx * r + j] = sum;
     }
@@ -330,7 +326,7 @@ cache_bwd_lr(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scal
                                            lane, s + o, ri + o, g + o, alpha + o, dq_acc);
         }
     }
-    store_dq(keys, dq_acc, stage, r_pad, partial, bx, wave, lane);  // (a barrier: LDS is written)
+    store_dq<kWaves>(keys, dq_acc, stage, r_pad, partial, bx, wave, lane);  // (a barrier: LDS is written)
     store_coef<OUT>(coef, lds, lds + array, lds + 2 * array, lds + 3 * array, s_pad, kWaves * P,
                     bx * kWaves * P, 0, S, N, 1.0f / (float)r, threadIdx.x, kBlock);
 }
@@ -355,8 +351,8 @@ cache_value_grads(const T *__restrict__ dH, const float *__restrict__ alpha, T *
 // The same for few tokens: one token a workgroup, its sources cut into a range a
 // wave, whose groups take every G-th one, U of them in flight a lane; scores and
 // dots of all of them meet in LDS.
-template <int FMT, typename T, int LG, int NCH, bool SLICED, CacheGrad OUT>
-__global__ void __launch_bounds__(kBlock)
+template <int FMT, typename T, int LG, int NCH, bool SLICED, CacheGrad OUT, int W>
+__global__ void __launch_bounds__(W * kWaveSize)
 cache_bwd_lr_wg(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                 const void *__restrict__ K, const float *__restrict__ q, const T *__restrict__ dH,
                 T *__restrict__ dV, T *__restrict__ dK, float *__restrict__ coef,
@@ -370,9 +366,9 @@ cache_bwd_lr_wg(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ s
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
     float *s = lds, *ri = s + s_pad, *g = ri + s_pad, *ds = g + s_pad;
     float *alpha = ds + s_pad + wave * s_pad;  // a wave's own
-    float *stage = lds + (4 + kWaves) * s_pad;
+    float *stage = lds + (4 + W) * s_pad;
     const int n = xcd_block().x;
-    const int per = (S + kWaves - 1) / kWaves;
+    const int per = (S + W - 1) / W;
     const int ib = min(S, wave * per), ie = min(S, ib + per);
     const Keys<FMT, T, SLICED> keys(K, codes, scales, N, d, r);
     const Lanes<FMT, LG, NCH> ln(lane, d);
@@ -440,13 +436,13 @@ cache_bwd_lr_wg(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ s
     for (int i = ib + lane; i < ie; i += kWaveSize)
         ds[i] = alpha[i] * (g[i] - gb);
     wave_lds_sync();
-    key_grads<FMT, T, SLICED, OUT>(keys, dhrow, dV, dK, qk, ib, ie, n, lane, s, ri, ds, alpha, dq_acc);
     if constexpr (OUT == kGradCoef)
         store_coef<OUT>(coef, s, ri, ds, alpha, 0, 1, n, ib, ie, N, 1.0f / (float)r, lane, kWaveSize);
     else
         value_grads<T, value_chunks<T>(NCH * LG * CW), OUT, 1>(
             dH, dV, ib, ie, n, N, d, SLICED ? keys.base : d, lane, alpha, 1, 0);
-    store_dq(keys, dq_acc, stage, r_pad, partial, n, wave, lane);
+    key_grads<FMT, T, SLICED, OUT>(keys, dhrow, dV, dK, qk, ib, ie, n, lane, s, ri, ds, alpha, dq_acc);
+    store_dq<W>(keys, dq_acc, stage, r_pad, partial, n, wave, lane);
 }
 
 // Full-rank keys: pass 1 reads the rows for sum(x^2), q.x and dH.x; pass 2 reads
@@ -613,8 +609,10 @@ struct CacheBwdPlan {
 };
 CacheBwdPlan cache_bwd_plan(const CacheProblem &p);
 
+// Workgroups that keep the write stream of the value rows busy.
+constexpr int kValueBlocks = 256;
 // Tokens a group of the low-rank backward where there are many, by chunks.
-constexpr int bwd_many(int nch) { return nch == 1 ? 4 : nch == 2 ? 2 : 1; }
+constexpr int bwd_many(int nch) { return nch <= 2 ? 4 : 2; }
 
 template <int FMT, typename T>
 hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, void *dK,
@@ -651,17 +649,26 @@ hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, 
                                    coef, partial, S, N, d, r, p.eps, s_pad, r_pad);
                 if constexpr (OUT != kGradCoef) {
                     constexpr int NO = value_chunks<T>(NCH * LG * unit_cols<FMT>());
-                    constexpr int TT = VAL_TT;
-                    const int per = VAL_PER, tokens = kWaves * TT;
-                    hipLaunchKernelGGL((cache_value_grads<T, NO, OUT, TT>),
-                                       dim3((unsigned)((N + tokens - 1) / tokens),
-                                            (unsigned)((S + per - 1) / per)),
-                                       dim3(kBlock), 0, st, dh, coef, dv, S, N, d,
-                                       SL ? (d - r) / 8 * 8 : d, per);
+                    auto rows = [&](auto tt) {
+                        constexpr int TT = decltype(tt)::value;
+                        const int tokens = kWaves * TT, gx = (N + tokens - 1) / tokens;
+                        // Source ranges, for at least kValueBlocks workgroups.
+                        const int parts = min(S, (kValueBlocks + gx - 1) / gx);
+                        const int per = (S + parts - 1) / parts;
+                        hipLaunchKernelGGL((cache_value_grads<T, NO, OUT, TT>),
+                                           dim3((unsigned)gx, (unsigned)((S + per - 1) / per)),
+                                           dim3(kBlock), 0, st, dh, coef, dv, S, N, d,
+                                           SL ? (d - r) / 8 * 8 : d, per);
+                    };
+                    constexpr int TM = NO <= 4 ? 8 : 4;
+                    if (N >= kValueBlocks * kWaves * TM)
+                        rows(std::integral_constant<int, TM>{});
+                    else
+                        rows(std::integral_constant<int, 2>{});
                 }
             };
             if (pl.split)
-                hipLaunchKernelGGL((cache_bwd_lr_wg<FMT, T, LG, NCH, SL, OUT>), dim3(pl.nblocks),
+                hipLaunchKernelGGL((cache_bwd_lr_wg<FMT, T, LG, NCH, SL, OUT, kWaves>), dim3(pl.nblocks),
                                    dim3(kBlock), ((4 + kWaves) * s_pad + kWaves * r_pad) * sizeof(float),
                                    st, p.codes, p.scales, p.K, p.q, dh, dv, dk, coef, partial, S, N,
                                    d, r, p.eps, s_pad, r_pad);

@@ -10,7 +10,7 @@ namespace {
 
 // Tokens up to which the low-rank backward splits each token's sources over a
 // workgroup.
-constexpr int64_t kSplitBwd = 512;
+constexpr int64_t kSplitBwd = 1024;
 // Waves from which a group takes several tokens (two a SIMD), and the sources up
 // to which their statistics fit LDS.
 constexpr int64_t kManyWaves = 2048, kManySources = 128;

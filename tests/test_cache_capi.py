@@ -230,8 +230,8 @@ def test_workspace_query(lib):
     q = lib.lr_attnres_cache_route_bwd_workspace_bytes
     for mode, r in ((P, 32), (SL, 32), (F, 512)):
         for N in (1, 511, 512, 513, 4095, 4096, 16384):
-            sizes = {q(S, N, 512, r, mode, FP8, BF16) for S in (1, 8, 9, 64)}
-            assert len(sizes) == 1 and sizes.pop() > 0
+            sizes = [q(S, N, 512, r, mode, FP8, BF16) for S in (1, 8, 9, 64, 129, 512)]
+            assert sizes == sorted(sizes) and sizes[0] > 0
     assert q(4, 0, 64, 8, SL, FP8, BF16) == 0
     assert q(4, 8, 64, 8, 9, FP8, BF16) == 0
     assert q(4, 8, 64, 8, SL, 7, BF16) == 0
@@ -301,5 +301,3 @@ def test_binding_refuses(lib):
         lr.cache_route_bwd(c, None, q, dH, "sliced", out=(O, None, q[:3]))
     with pytest.raises(ValueError, match="coef must be"):
         lr.cache_route_bwd_deferred(c, None, q, dH, "sliced", torch.zeros(3, 5, 3))
-    with pytest.raises(ValueError, match="all tensors"):
-        lr.cache_route_fwd(c, None, q.to("meta"), "sliced")
