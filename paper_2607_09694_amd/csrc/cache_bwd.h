@@ -131,20 +131,20 @@ __device__ __forceinline__ void value_grads(const T *__restrict__ dH, T *__restr
 {
     constexpr int VO = 16 / sizeof(T);
     u32x4_t dh[TT][NO];
-    int n[TT];
+    const int nt = min(TT, N - n0);  // wave-uniform
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
-        n[t] = min(n0 + t, N - 1);  // tokens past the end: the last one again, the same values
+    for (int t = 0; t < TT; ++t)
 #pragma unroll
         for (int c = 0; c < NO; ++c)
-            dh[t][c] = load16_elems(dH + (size_t)n[t] * d, (c * kWaveSize + lane) * VO, d);
-    }
+            dh[t][c] = load16_elems(dH + (size_t)(n0 + min(t, nt - 1)) * d, (c * kWaveSize + lane) * VO, d);
     for (int i = ib; i < ie; ++i) {
         T *plane = dV + (size_t)i * N * d;
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
-            const float a = alpha[i * si + (n[t] - n0) * st];
-            T *orow = plane + (size_t)n[t] * d;
+            if (t >= nt)
+                break;
+            const float a = alpha[i * si + t * st];
+            T *orow = plane + (size_t)(n0 + t) * d;
 #pragma unroll
             for (int c = 0; c < NO; ++c) {
                 const int col = (c * kWaveSize + lane) * VO;
@@ -445,160 +445,237 @@ cache_bwd_lr_wg(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ s
     store_dq<W>(keys, dq_acc, stage, r_pad, partial, n, wave, lane);
 }
 
-// Full-rank keys: pass 1 reads the rows for sum(x^2), q.x and dH.x; pass 2 reads
-// them again for dV_i = alpha_i dH + (ds_i / rho_i)(q - x_i s_i / (rho_i d)) and
-// dq.  Every group of lanes has a token of its own, tpw in turn.
+// VO = 16 / sizeof(T) consecutive columns of a cache row, as a lane that writes 16
+// bytes of a gradient row reads them.
+template <int FMT, int VO> struct OutCodes {
+    typedef std::conditional_t<VO * 2 / Codes<FMT>::per_byte == 16, u32x2_t,
+                               std::conditional_t<VO * 2 / Codes<FMT>::per_byte == 8, unsigned, uint16_t>>
+        code_t;
+    code_t c;
+    unsigned e;
+    // Columns col .. of the row `row` (columns past its last block: that block's).
+    __device__ __forceinline__ void load(const uint8_t *__restrict__ codes,
+                                         const uint8_t *__restrict__ scales, size_t row, int nb, int col)
+    {
+        col = min(col, nb * kCacheBlock - VO);
+        c = *reinterpret_cast<const code_t *>(codes + (row * nb * kCacheBlock) / Codes<FMT>::per_byte +
+                                              (unsigned)(col / Codes<FMT>::per_byte));
+        e = scales[row * nb + (unsigned)col / kCacheBlock];
+    }
+    __device__ __forceinline__ void values(float (&x)[VO]) const
+    {
+        const float sc = block_scale(e);
+        float y[8];
+        if constexpr (VO == 8) {
+            decode<FMT>(c, sc, y);
+        } else if constexpr (FMT == LRAR_CACHE_FP8) {
+            decode_fp8(c, sc, y);
+        } else {
+            decode_fp4(c, sc, y);
+        }
+#pragma unroll
+        for (int k = 0; k < VO; ++k)
+            x[k] = y[k];
+    }
+};
+
+// Full-rank keys: one token a workgroup at a time (tpw in turn).  Pass 1 deals its
+// sources to the waves' groups of lanes and forms sum(x^2), q.x and dH.x, which
+// meet in LDS; pass 2 deals them to the waves, reads the rows again (from the L2)
+// in the layout of the gradient rows, whole lines a store, and writes
+//     dV_i = alpha_i dH + (ds_i / rho_i)(q - x_i s_i / (rho_i d)),
+// adding (ds_i / rho_i) x_i to dq.  (Storing from the layout of pass 1, 16 bytes a
+// lane 32 or 64 bytes apart, took 1.3 times as long.)
 template <int FMT, typename T, int LG, int NCH, bool ADD>
 __global__ void __launch_bounds__(kBlock)
 cache_bwd_full(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                const float *__restrict__ q, const T *__restrict__ dH, T *__restrict__ dV,
                float *__restrict__ partial, int S, int N, int d, float eps, int s_pad, int tpw)
 {
-    constexpr int G = kWaveSize / LG, CW = unit_cols<FMT>(), kRow = NCH * LG * CW;
+    constexpr int G = kWaveSize / LG, CW = unit_cols<FMT>(), GG = kWaves * G;
     constexpr int per = kCacheBlock / CW;  // units a block
+    constexpr int U = NCH >= 4 ? 4 : 8;
+    constexpr int VO = 16 / sizeof(T), NO = value_chunks<T>(NCH * LG * CW), B = NO >= 8 ? 2 : 4;
     extern __shared__ float lds[];
     const int lane = threadIdx.x & (kWaveSize - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
     const Lanes<FMT, LG, NCH> ln(lane, d);
-    float *sc = lds + (wave * G + ln.g) * 4 * s_pad;  // the group's scores
-    float *ri = sc + s_pad, *g = ri + s_pad, *alpha = g + s_pad;
-    float *stage = lds + kWaves * G * 4 * s_pad;      // [kRow]
+    float *sc = lds, *ri = sc + s_pad, *g = ri + s_pad;
+    float *alpha = g + s_pad + wave * s_pad;   // a wave's own
+    float *stage = lds + (3 + kWaves) * s_pad;  // [NO * 64 * VO]
     const float inv_d = 1.0f / (float)d;
-    float qv[NCH][CW], dqa[NCH][CW];
+    const int i1 = wave * G + ln.g;  // a group's first source; every GG-th follows
+    // The query in LDS: both passes read it in their own layout, and hold it only
+    // while they run.
+    float *ql = stage + NO * kWaveSize * VO;  // [NO * 64 * VO]
+    for (int j = threadIdx.x; j < NO * kWaveSize * VO; j += kBlock)
+        ql[j] = j < d ? q[j] : 0.0f;
+    __syncthreads();
+    float dqa[NO][VO];
 #pragma unroll
-    for (int c = 0; c < NCH; ++c)
+    for (int c = 0; c < NO; ++c)
 #pragma unroll
-        for (int e = 0; e < CW; ++e) {
-            const int j = ln.col(c) + e;
-            qv[c][e] = j < d ? q[j] : 0.0f;
+        for (int e = 0; e < VO; ++e)
             dqa[c][e] = 0.0f;
-        }
     const size_t plane = (size_t)N * ln.nu;
+    const int nb = (d + kCacheBlock - 1) / kCacheBlock;
     const int bx = xcd_block().x;
     for (int t = 0; t < tpw; ++t) {
-        const int n0 = ((bx * tpw + t) * kWaves + wave) * G;
-        if (n0 >= N)
-            break;  // wave-uniform; the workgroup barriers are after the loop
-        const bool live = n0 + ln.g < N;  // a group past the last token adds and writes nothing
-        const int n = min(n0 + ln.g, N - 1);
-        const size_t first = (size_t)n0 * ln.nu;
-        unsigned at[NCH];
-        float dh[NCH][CW];
-        load_dh<FMT, T, LG, NCH>(dH + (size_t)n * d, ln, d, dh);
+        const int n = bx * tpw + t;
+        if (n >= N)
+            break;  // workgroup-uniform
+        const size_t first = (size_t)n * ln.nu;
+        UnitRaw<FMT> w[U][NCH];
+        auto load = [&](int i0) {
 #pragma unroll
-        for (int c = 0; c < NCH; ++c)
-            at[c] = ln.at[c] + (unsigned)((n - n0) * ln.nu);
-        for (int i0 = 0; i0 < S; i0 += 4) {
-            UnitRaw<FMT> w[4][NCH];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const size_t b = min(i0 + u, S - 1) * plane + first;
+            for (int u = 0; u < U; ++u) {
+                const size_t b = min(i0 + u * GG + i1, S - 1) * plane + first;
 #pragma unroll
                 for (int c = 0; c < NCH; ++c)
-                    load_unit<FMT>(codes + b * 16, scales + b / per, at[c], w[u][c]);
+                    load_unit<FMT>(codes + b * 16, scales + b / per, ln.at[c], w[u][c]);
             }
+        };
+        float dh[NCH][CW], qv[NCH][CW];
+        load_dh<FMT, T, LG, NCH>(dH + (size_t)n * d, ln, d, dh);
+        load(0);
+#pragma unroll
+        for (int c = 0; c < NCH; ++c)
+#pragma unroll
+            for (int e = 0; e < CW; e += 4) {
+                const f32x4_t x = *reinterpret_cast<const f32x4_t *>(ql + ln.col(c) + e);
+                qv[c][e] = x.x; qv[c][e + 1] = x.y; qv[c][e + 2] = x.z; qv[c][e + 3] = x.w;
+            }
+        for (int i0 = 0; i0 < S; i0 += U * GG) {
+            if (i0 > 0)
+                load(i0);
             __builtin_amdgcn_sched_barrier(0);
-            float ss[4], dot[4], p[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                ss[u] = dot[u] = p[u] = 0.0f;
+            for (int v = 0; v < U; v += 4) {
+                if (i0 + v * GG >= S)
+                    break;  // uniform
+                float ss[4], dot[4], p[4];
 #pragma unroll
-                for (int c = 0; c < NCH; ++c) {
-                    float a = 0.0f;
+                for (int u = 0; u < 4; ++u) {
+                    ss[u] = dot[u] = p[u] = 0.0f;
 #pragma unroll
-                    for (int h = 0; h < CW / 16; ++h) {
-                        float x[16];
-                        unit_values<FMT>(w[u][c], h, x);
+                    for (int c = 0; c < NCH; ++c) {
+                        float a = 0.0f;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            a = fmaf(x[e], x[e], a);
-                            dot[u] = fmaf(qv[c][16 * h + e], x[e], dot[u]);
-                            p[u] = fmaf(dh[c][16 * h + e], x[e], p[u]);
+                        for (int h = 0; h < CW / 16; ++h) {
+                            float x[16];
+                            unit_values<FMT>(w[v + u][c], h, x);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                a = fmaf(x[e], x[e], a);
+                                dot[u] = fmaf(qv[c][16 * h + e], x[e], dot[u]);
+                                p[u] = fmaf(dh[c][16 * h + e], x[e], p[u]);
+                            }
                         }
+                        ss[u] += ln.in[c] ? a : 0.0f;
                     }
-                    ss[u] += ln.in[c] ? a : 0.0f;
+                }
+                const float tss = four_sums<LG>(ss, lane), tdot = four_sums<LG>(dot, lane),
+                            tg = four_sums<LG>(p, lane);
+                const int i = i0 + (v + four_index<LG>(lane)) * GG + i1;
+                if (lane % (LG / 4) == 0 && i < S) {
+                    const float rv = rsqrtf(tss * inv_d + eps);
+                    ri[i] = rv;
+                    sc[i] = tdot * rv;
+                    g[i] = tg;
                 }
             }
-            const float tss = four_sums<LG>(ss, lane), tdot = four_sums<LG>(dot, lane),
-                        tg = four_sums<LG>(p, lane);
-            const int i = i0 + four_index<LG>(lane);
-            if (lane % (LG / 4) == 0 && i < S) {
-                const float rv = rsqrtf(tss * inv_d + eps);
-                ri[i] = rv;
-                sc[i] = tdot * rv;
-                g[i] = tg;
-            }
         }
-        wave_lds_sync();
-        group_softmax<LG>(sc, alpha, 0, S, 0, ln.lu);
-        float gb = 0.0f;
-        for (int i = ln.lu; i < S; i += LG)
-            gb = fmaf(alpha[i], g[i], gb);
-        gb = group_sum(gb, LG);
-        for (int i = ln.lu; i < S; i += LG)
-            g[i] = alpha[i] * (g[i] - gb);
+        __syncthreads();
+        float m = -INFINITY, z = 0.0f, gb = 0.0f;
+        for (int i = lane; i < S; i += kWaveSize)
+            m = fmaxf(m, sc[i]);
+        m = group_max(m, kWaveSize);
+        for (int i = lane; i < S; i += kWaveSize) {
+            const float e = expf(sc[i] - m);
+            alpha[i] = e;
+            z += e;
+        }
+        const float inv = 1.0f / group_sum(z, kWaveSize);
+        for (int i = lane; i < S; i += kWaveSize) {
+            const float a = alpha[i] * inv;
+            alpha[i] = a;
+            gb = fmaf(a, g[i], gb);
+        }
+        gb = group_sum(gb, kWaveSize);
         wave_lds_sync();
 
-        for (int i = 0; i < S; ++i) {
-            const float a = alpha[i];
-            const float c1 = live ? g[i] * ri[i] : 0.0f;     // ds_i / rho_i
-            const float c2 = c1 * sc[i] * ri[i] * inv_d;     // ds_i s_i / (rho_i^2 d)
-            T *orow = dV + ((size_t)i * N + n) * d;
-            UnitRaw<FMT> w[NCH];
-            const size_t b = i * plane + first;
+        float dho[NO][VO], qo[NO][VO];
 #pragma unroll
-            for (int c = 0; c < NCH; ++c)
-                load_unit<FMT>(codes + b * 16, scales + b / per, at[c], w[c]);
+        for (int c = 0; c < NO; ++c) {
+            const int col = (c * kWaveSize + lane) * VO;
+            const u32x4_t r = load16_elems(dH + (size_t)n * d, col, d);
+            if constexpr (VO == 8)
+                widen(r, dho[c]);
+            else
+                widen(__builtin_bit_cast(f32x4_t, r), dho[c]);
 #pragma unroll
-            for (int c = 0; c < NCH; ++c)
-#pragma unroll
-                for (int h = 0; h < CW / 16; ++h) {
-                    float x[16];
-                    unit_values<FMT>(w[c], h, x);
-#pragma unroll
-                    for (int hh = 0; hh < 2; ++hh) {
-                        const int oc = ln.col(c) + 16 * h + 8 * hh;
-                        float y[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const int k = 16 * h + 8 * hh + e;
-                            const float xe = x[8 * hh + e];
-                            y[e] = fmaf(a, dh[c][k], fmaf(c1, qv[c][k], -c2 * xe));
-                            dqa[c][k] = fmaf(c1, xe, dqa[c][k]);
-                        }
-                        if (live) {
-                            if constexpr (ADD) {
-                                float o[8];
-                                load8(orow, oc, d, o);
-#pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    y[e] += o[e];
-                            }
-                            store8<T, false>(orow, oc, d, y);
-                        }
-                    }
-                }
+            for (int e = 0; e < VO; ++e)
+                qo[c][e] = ql[col + e];
         }
-        wave_lds_sync();
+        for (int i0 = wave; i0 < S; i0 += B * kWaves) {
+            OutCodes<FMT, VO> z[B][NO];
+#pragma unroll
+            for (int u = 0; u < B; ++u)
+#pragma unroll
+                for (int c = 0; c < NO; ++c)
+                    z[u][c].load(codes, scales, (size_t)min(i0 + u * kWaves, S - 1) * N + n, nb,
+                                 (c * kWaveSize + lane) * VO);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < B; ++u) {
+                const int i = i0 + u * kWaves;
+                if (i >= S)
+                    break;  // wave-uniform
+                const float a = alpha[i];
+                const float c1 = a * (g[i] - gb) * ri[i];      // ds_i / rho_i
+                const float c2 = c1 * sc[i] * ri[i] * inv_d;   // ds_i s_i / (rho_i^2 d)
+                T *orow = dV + ((size_t)i * N + n) * d;
+#pragma unroll
+                for (int c = 0; c < NO; ++c) {
+                    const int col = (c * kWaveSize + lane) * VO;
+                    float x[VO], y[VO];
+                    z[u][c].values(x);
+#pragma unroll
+                    for (int e = 0; e < VO; ++e) {
+                        y[e] = fmaf(a, dho[c][e], fmaf(c1, qo[c][e], -c2 * x[e]));
+                        dqa[c][e] = fmaf(c1, x[e], dqa[c][e]);
+                    }
+                    if constexpr (ADD) {
+                        const u32x4_t o = load16_elems(orow, col, d);
+                        if constexpr (VO == 8)
+                            add_stored(y, o);
+                        else
+                            add_stored(y, __builtin_bit_cast(f32x4_t, o));
+                    }
+                    store16_elems<T, kBwdNtStore>(orow, col, d,
+                                                  __builtin_bit_cast(u32x4_t, Narrow<T, VO>::run(y)));
+                }
+            }
+        }
+        __syncthreads();  // LDS of this token is reused by the next one
     }
-    // dq: the groups and waves add their columns in turn.
-    for (int w = 0; w < kWaves * G; ++w) {
-        if (wave * G + ln.g == w) {
+    // dq: the waves add their columns in turn.
+    for (int w = 0; w < kWaves; ++w) {
+        if (wave == w) {
 #pragma unroll
-            for (int c = 0; c < NCH; ++c)
+            for (int c = 0; c < NO; ++c)
 #pragma unroll
-                for (int e = 0; e < CW; ++e) {
-                    float *p = stage + (c * CW + e) * LG + ln.lu;
+                for (int e = 0; e < VO; ++e) {
+                    float *p = stage + (c * VO + e) * kWaveSize + lane;
                     *p = (w == 0 ? 0.0f : *p) + dqa[c][e];
                 }
         }
         __syncthreads();
     }
     for (int j = threadIdx.x; j < d; j += kBlock) {
-        const int unit = j / CW, e = j % CW;  // unit = lu + c LG
-        partial[(size_t)bx * d + j] = stage[(unit / LG * CW + e) * LG + unit % LG];
+        const int at = j / VO, e = j % VO;  // at = c * 64 + lane
+        partial[(size_t)bx * d + j] = stage[(at / kWaveSize * VO + e) * kWaveSize + at % kWaveSize];
     }
-    static_assert(kRow >= LG, "");
 }
 
 // How a backward is laid out over workgroups.
@@ -627,15 +704,17 @@ hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, 
     return dispatch_lanes<FMT>(p.d, [&](auto lg, auto nc) -> hipError_t {
         constexpr int LG = decltype(lg)::value, NCH = decltype(nc)::value, G = kWaveSize / LG;
         if (p.mode == LRAR_MODE_FULL) {
-            const size_t lds = ((size_t)kWaves * G * 4 * s_pad + NCH * LG * unit_cols<FMT>()) * sizeof(float);
+            const int s4 = (S + 3) / 4 * 4;  // 16-byte aligned rows behind the scores
+            const size_t lds = ((size_t)(3 + kWaves) * s4 +
+                                2 * value_chunks<T>(NCH * LG * unit_cols<FMT>()) * (1024 / sizeof(T))) * sizeof(float);
             if (accumulate)
                 hipLaunchKernelGGL((cache_bwd_full<FMT, T, LG, NCH, true>), dim3(pl.nblocks),
                                    dim3(kBlock), lds, st, p.codes, p.scales, p.q, dh, dv, partial,
-                                   S, N, d, p.eps, s_pad, pl.tpw);
+                                   S, N, d, p.eps, s4, pl.tpw);
             else
                 hipLaunchKernelGGL((cache_bwd_full<FMT, T, LG, NCH, false>), dim3(pl.nblocks),
                                    dim3(kBlock), lds, st, p.codes, p.scales, p.q, dh, dv, partial,
-                                   S, N, d, p.eps, s_pad, pl.tpw);
+                                   S, N, d, p.eps, s4, pl.tpw);
             return hipGetLastError();
         }
         auto by_form = [&](auto sliced, auto out) {

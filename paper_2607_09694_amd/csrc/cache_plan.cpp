@@ -14,6 +14,9 @@ constexpr int64_t kSplitBwd = 1024;
 // Waves from which a group takes several tokens (two a SIMD), and the sources up
 // to which their statistics fit LDS.
 constexpr int64_t kManyWaves = 2048, kManySources = 128;
+// Workgroups from which one of full-rank keys takes several tokens in turn, for
+// fewer rows of dq partials.
+constexpr int64_t kFullBlocks = 512;
 
 }  // namespace
 
@@ -26,8 +29,8 @@ CacheBwdPlan cache_bwd_plan(const CacheProblem &p)
     const int many = bwd_many(units <= 64 ? 1 : units <= 128 ? 2 : 4);
     pl.split = !full && p.N <= kSplitBwd;
     pl.many = !full && !pl.split && p.S <= kManySources && p.N >= kManyWaves * groups * many;
-    pl.tpw = !full ? 1 : p.N >= 4096 * groups ? 4 : 1;
-    const int64_t per = pl.split ? 1 : kWaves * groups * (pl.many ? many : pl.tpw);
+    pl.tpw = !full ? 1 : p.N >= 4 * kFullBlocks ? 4 : p.N >= 2 * kFullBlocks ? 2 : 1;
+    const int64_t per = full ? pl.tpw : pl.split ? 1 : kWaves * groups * (pl.many ? many : 1);
     pl.nblocks = (int)((p.N + per - 1) / per);
     return pl;
 }
