@@ -12,6 +12,7 @@
 #pragma once
 
 #include "cache_device.h"
+#include "cache_full.h"
 
 namespace lrar {
 
@@ -190,7 +191,7 @@ __device__ __forceinline__ void store_dq(const Keys<FMT, T, SLICED> &keys, float
             if (j + e >= 0 && j + e < r)
                 my[j + e] = dq_acc[e];
     }
-    __syncthreads();
+    lds_barrier();
     for (int j = threadIdx.x; j < r; j += W * kWaveSize) {
         float sum = 0.0f;
         for (int w = 0; w < W; ++w)
@@ -415,7 +416,7 @@ cache_bwd_lr_wg(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ s
             }
         }
     }
-    __syncthreads();
+    lds_barrier();
     float m = -INFINITY, z = 0.0f, gb = 0.0f;
     for (int i = lane; i < S; i += kWaveSize)
         m = fmaxf(m, s[i]);
@@ -480,112 +481,62 @@ template <int FMT, int VO> struct OutCodes {
 };
 
 // Full-rank keys: one token a workgroup at a time (tpw in turn).  Pass 1 deals its
-// sources to the waves' groups of lanes and forms sum(x^2), q.x and dH.x, which
-// meet in LDS; pass 2 deals them to the waves, reads the rows again (from the L2)
-// in the layout of the gradient rows, whole lines a store, and writes
+// sources in tiles of 16 to the waves, which form |x|^2, q.x and dH.x on the matrix
+// cores; these meet in LDS.  Pass 2 deals the sources to the waves, reads the rows
+// again (from the L2) in the layout of the gradient rows, whole lines a store, and
+// writes
 //     dV_i = alpha_i dH + (ds_i / rho_i)(q - x_i s_i / (rho_i d)),
-// adding (ds_i / rho_i) x_i to dq.  (Storing from the layout of pass 1, 16 bytes a
-// lane 32 or 64 bytes apart, took 1.3 times as long.)
-template <int FMT, typename T, int LG, int NCH, bool ADD>
+// adding (ds_i / rho_i) x_i to dq.
+template <int FMT, typename T, int NO, bool ADD>
 __global__ void __launch_bounds__(kBlock)
 cache_bwd_full(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                const float *__restrict__ q, const T *__restrict__ dH, T *__restrict__ dV,
                float *__restrict__ partial, int S, int N, int d, float eps, int s_pad, int tpw)
 {
-    constexpr int G = kWaveSize / LG, CW = unit_cols<FMT>(), GG = kWaves * G;
-    constexpr int per = kCacheBlock / CW;  // units a block
-    constexpr int U = NCH >= 4 ? 4 : 8;
-    constexpr int VO = 16 / sizeof(T), NO = value_chunks<T>(NCH * LG * CW), B = NO >= 8 ? 2 : 4;
+    constexpr int VO = 16 / sizeof(T), B = NO >= 8 ? 2 : 4;
     extern __shared__ float lds[];
     const int lane = threadIdx.x & (kWaveSize - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
-    const Lanes<FMT, LG, NCH> ln(lane, d);
+    // Of every chunk of columns q.x, |x|^2 and dH.x of the sources; then, in the first
+    // chunk's place, the scores, 1 / rho and dH.x.
     float *sc = lds, *ri = sc + s_pad, *g = ri + s_pad;
-    float *alpha = g + s_pad + wave * s_pad;   // a wave's own
-    float *stage = lds + (3 + kWaves) * s_pad;  // [NO * 64 * VO]
+    const int parts = 3 * tile_chunks<FMT>(d);
+    float *alpha = lds + (parts + wave) * s_pad;    // a wave's own
+    float *stage = lds + (parts + kWaves) * s_pad;  // [NO * 64 * VO]: q, at the end dq
+    uint8_t *qop = reinterpret_cast<uint8_t *>(stage + NO * kWaveSize * VO);
+    uint8_t *dop = qop + operand_bytes<FMT>(d);
+    uint8_t *tile = dop + operand_bytes<FMT>(d) + wave * kTileBytes;
     const float inv_d = 1.0f / (float)d;
-    const int i1 = wave * G + ln.g;  // a group's first source; every GG-th follows
-    // The query in LDS: both passes read it in their own layout, and hold it only
-    // while they run.
-    float *ql = stage + NO * kWaveSize * VO;  // [NO * 64 * VO]
+    const int nb = (d + kCacheBlock - 1) / kCacheBlock;
+    float *ql = stage;
     for (int j = threadIdx.x; j < NO * kWaveSize * VO; j += kBlock)
         ql[j] = j < d ? q[j] : 0.0f;
-    __syncthreads();
+    make_operand<FMT>(q, d, qop, threadIdx.x, kBlock);
+    // (The first token's barrier orders both.)
     float dqa[NO][VO];
 #pragma unroll
     for (int c = 0; c < NO; ++c)
 #pragma unroll
         for (int e = 0; e < VO; ++e)
             dqa[c][e] = 0.0f;
-    const size_t plane = (size_t)N * ln.nu;
-    const int nb = (d + kCacheBlock - 1) / kCacheBlock;
     const int bx = xcd_block().x;
     for (int t = 0; t < tpw; ++t) {
         const int n = bx * tpw + t;
         if (n >= N)
             break;  // workgroup-uniform
-        const size_t first = (size_t)n * ln.nu;
-        UnitRaw<FMT> w[U][NCH];
-        auto load = [&](int i0) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const size_t b = min(i0 + u * GG + i1, S - 1) * plane + first;
-#pragma unroll
-                for (int c = 0; c < NCH; ++c)
-                    load_unit<FMT>(codes + b * 16, scales + b / per, ln.at[c], w[u][c]);
-            }
-        };
-        float dh[NCH][CW], qv[NCH][CW];
-        load_dh<FMT, T, LG, NCH>(dH + (size_t)n * d, ln, d, dh);
-        load(0);
-#pragma unroll
-        for (int c = 0; c < NCH; ++c)
-#pragma unroll
-            for (int e = 0; e < CW; e += 4) {
-                const f32x4_t x = *reinterpret_cast<const f32x4_t *>(ql + ln.col(c) + e);
-                qv[c][e] = x.x; qv[c][e + 1] = x.y; qv[c][e + 2] = x.z; qv[c][e + 3] = x.w;
-            }
-        for (int i0 = 0; i0 < S; i0 += U * GG) {
-            if (i0 > 0)
-                load(i0);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int v = 0; v < U; v += 4) {
-                if (i0 + v * GG >= S)
-                    break;  // uniform
-                float ss[4], dot[4], p[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    ss[u] = dot[u] = p[u] = 0.0f;
-#pragma unroll
-                    for (int c = 0; c < NCH; ++c) {
-                        float a = 0.0f;
-#pragma unroll
-                        for (int h = 0; h < CW / 16; ++h) {
-                            float x[16];
-                            unit_values<FMT>(w[v + u][c], h, x);
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                a = fmaf(x[e], x[e], a);
-                                dot[u] = fmaf(qv[c][16 * h + e], x[e], dot[u]);
-                                p[u] = fmaf(dh[c][16 * h + e], x[e], p[u]);
-                            }
-                        }
-                        ss[u] += ln.in[c] ? a : 0.0f;
-                    }
-                }
-                const float tss = four_sums<LG>(ss, lane), tdot = four_sums<LG>(dot, lane),
-                            tg = four_sums<LG>(p, lane);
-                const int i = i0 + (v + four_index<LG>(lane)) * GG + i1;
-                if (lane % (LG / 4) == 0 && i < S) {
-                    const float rv = rsqrtf(tss * inv_d + eps);
-                    ri[i] = rv;
-                    sc[i] = tdot * rv;
-                    g[i] = tg;
-                }
-            }
+        make_operand<FMT>(dH + (size_t)n * d, d, dop, threadIdx.x, kBlock);
+        lds_barrier();
+        tile_dots<FMT, true>(codes, scales, n, N, 0, S, d, qop, dop, tile, wave, kWaves, lane, sc, s_pad);
+        lds_barrier();
+        const int chunks = tile_chunks<FMT>(d);
+        for (int i = threadIdx.x; i < S; i += kBlock) {
+            const float rv = rsqrtf(chunk_sum(sc, s_pad, chunks, 1, i) * inv_d + eps);
+            const float dot = chunk_sum(sc, s_pad, chunks, 0, i), gi = chunk_sum(sc, s_pad, chunks, 2, i);
+            sc[i] = dot * rv;
+            ri[i] = rv;
+            g[i] = gi;
         }
-        __syncthreads();
+        lds_barrier();
         float m = -INFINITY, z = 0.0f, gb = 0.0f;
         for (int i = lane; i < S; i += kWaveSize)
             m = fmaxf(m, sc[i]);
@@ -657,7 +608,7 @@ cache_bwd_full(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ sc
                 }
             }
         }
-        __syncthreads();  // LDS of this token is reused by the next one
+        lds_barrier();  // LDS of this token is reused by the next one
     }
     // dq: the waves add their columns in turn.
     for (int w = 0; w < kWaves; ++w) {
@@ -670,7 +621,7 @@ cache_bwd_full(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ sc
                     *p = (w == 0 ? 0.0f : *p) + dqa[c][e];
                 }
         }
-        __syncthreads();
+        lds_barrier();
     }
     for (int j = threadIdx.x; j < d; j += kBlock) {
         const int at = j / VO, e = j % VO;  // at = c * 64 + lane
@@ -704,17 +655,19 @@ hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, 
     return dispatch_lanes<FMT>(p.d, [&](auto lg, auto nc) -> hipError_t {
         constexpr int LG = decltype(lg)::value, NCH = decltype(nc)::value, G = kWaveSize / LG;
         if (p.mode == LRAR_MODE_FULL) {
+            constexpr int NO = value_chunks<T>(NCH * LG * unit_cols<FMT>());
             const int s4 = (S + 3) / 4 * 4;  // 16-byte aligned rows behind the scores
-            const size_t lds = ((size_t)(3 + kWaves) * s4 +
-                                2 * value_chunks<T>(NCH * LG * unit_cols<FMT>()) * (1024 / sizeof(T))) * sizeof(float);
+            const size_t lds = ((size_t)(3 * tile_chunks<FMT>(d) + kWaves) * s4 + NO * (1024 / sizeof(T))) * sizeof(float) +
+                               2 * operand_bytes<FMT>(d) + kWaves * kTileBytes;
+            auto launch = [&](auto add) {
+                hipLaunchKernelGGL((cache_bwd_full<FMT, T, NO, decltype(add)::value>), dim3(pl.nblocks),
+                                   dim3(kBlock), lds, st, p.codes, p.scales, p.q, dh, dv, partial, S, N,
+                                   d, p.eps, s4, pl.tpw);
+            };
             if (accumulate)
-                hipLaunchKernelGGL((cache_bwd_full<FMT, T, LG, NCH, true>), dim3(pl.nblocks),
-                                   dim3(kBlock), lds, st, p.codes, p.scales, p.q, dh, dv, partial,
-                                   S, N, d, p.eps, s4, pl.tpw);
+                launch(std::true_type{});
             else
-                hipLaunchKernelGGL((cache_bwd_full<FMT, T, LG, NCH, false>), dim3(pl.nblocks),
-                                   dim3(kBlock), lds, st, p.codes, p.scales, p.q, dh, dv, partial,
-                                   S, N, d, p.eps, s4, pl.tpw);
+                launch(std::false_type{});
             return hipGetLastError();
         }
         auto by_form = [&](auto sliced, auto out) {

@@ -64,7 +64,7 @@ __device__ __forceinline__ void merge_store(float (&acc)[NCH][UnitRaw<FMT>::cols
         for (int e = 0; e < CW / G; e += 4)
             *reinterpret_cast<f32x4_t *>(dst + e) = f32x4_t{v[e], v[e + 1], v[e + 2], v[e + 3]};
     }
-    __syncthreads();
+    lds_barrier();
     float mg = stat[0];
 #pragma unroll
     for (int u = 1; u < W; ++u)
