@@ -480,39 +480,52 @@ template <int FMT, int VO> struct OutCodes {
     }
 };
 
-// Full-rank keys: one token a workgroup at a time (tpw in turn).  Pass 1 deals its
-// sources in tiles of 16 to the waves, which form |x|^2, q.x and dH.x on the matrix
-// cores; these meet in LDS.  Pass 2 deals the sources to the waves, reads the rows
-// again (from the L2) in the layout of the gradient rows, whole lines a store, and
-// writes
+// Rows of s_pad floats that hold the dots of a token's sources.
+template <int FMT> constexpr int full_parts(int d)
+{
+    return FMT == LRAR_CACHE_FP4 ? 3 * tile_chunks(d) : 3;
+}
+
+// Full-rank keys: one token a workgroup at a time (tpw in turn).  Pass 1 forms
+// |x|^2, q.x and dH.x of its sources, which meet in LDS: e2m1 rows on the matrix
+// cores (tile_dots), e4m3 rows dealt to the waves' groups of lanes.  Pass 2 deals
+// the sources to the waves, reads the rows again (from the L2) in the layout of the
+// gradient rows, whole lines a store, and writes
 //     dV_i = alpha_i dH + (ds_i / rho_i)(q - x_i s_i / (rho_i d)),
 // adding (ds_i / rho_i) x_i to dq.
-template <int FMT, typename T, int NO, bool ADD>
+template <int FMT, typename T, int LG, int NCH, bool ADD>
 __global__ void __launch_bounds__(kBlock)
 cache_bwd_full(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                const float *__restrict__ q, const T *__restrict__ dH, T *__restrict__ dV,
                float *__restrict__ partial, int S, int N, int d, float eps, int s_pad, int tpw)
 {
-    constexpr int VO = 16 / sizeof(T), B = NO >= 8 ? 2 : 4;
+    constexpr int G = kWaveSize / LG, CW = unit_cols<FMT>(), GG = kWaves * G;
+    constexpr int per = kCacheBlock / CW;  // units a block
+    constexpr int VO = 16 / sizeof(T), NO = value_chunks<T>(NCH * LG * CW), B = NO >= 8 ? 2 : 4;
+    constexpr bool TILES = FMT == LRAR_CACHE_FP4;
     extern __shared__ float lds[];
     const int lane = threadIdx.x & (kWaveSize - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
-    // Of every chunk of columns q.x, |x|^2 and dH.x of the sources; then, in the first
-    // chunk's place, the scores, 1 / rho and dH.x.
+    const Lanes<FMT, LG, NCH> ln(lane, d);
+    // The scores, 1 / rho and dH.x of the sources (before that, of every chunk of
+    // columns q.x, |x|^2 and dH.x).
     float *sc = lds, *ri = sc + s_pad, *g = ri + s_pad;
-    const int parts = 3 * tile_chunks<FMT>(d);
+    const int parts = full_parts<FMT>(d);
     float *alpha = lds + (parts + wave) * s_pad;    // a wave's own
     float *stage = lds + (parts + kWaves) * s_pad;  // [NO * 64 * VO]: q, at the end dq
-    uint8_t *qop = reinterpret_cast<uint8_t *>(stage + NO * kWaveSize * VO);
-    uint8_t *dop = qop + operand_bytes<FMT>(d);
-    uint8_t *tile = dop + operand_bytes<FMT>(d) + wave * kTileBytes;
+    uint8_t *qop = reinterpret_cast<uint8_t *>(stage + NO * kWaveSize * VO);  // TILES: operands, tiles
+    uint8_t *dop = qop + operand_bytes(d);
+    uint8_t *tile = dop + operand_bytes(d) + wave * kTileBytes;
     const float inv_d = 1.0f / (float)d;
     const int nb = (d + kCacheBlock - 1) / kCacheBlock;
+    // The query in LDS: both passes read it in their own layout, and hold it only
+    // while they run.
     float *ql = stage;
     for (int j = threadIdx.x; j < NO * kWaveSize * VO; j += kBlock)
         ql[j] = j < d ? q[j] : 0.0f;
-    make_operand<FMT>(q, d, qop, threadIdx.x, kBlock);
-    // (The first token's barrier orders both.)
+    if constexpr (TILES)
+        make_operand(q, d, qop, threadIdx.x, kBlock);
+    lds_barrier();
     float dqa[NO][VO];
 #pragma unroll
     for (int c = 0; c < NO; ++c)
@@ -524,17 +537,79 @@ cache_bwd_full(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ sc
         const int n = bx * tpw + t;
         if (n >= N)
             break;  // workgroup-uniform
-        make_operand<FMT>(dH + (size_t)n * d, d, dop, threadIdx.x, kBlock);
-        lds_barrier();
-        tile_dots<FMT, true>(codes, scales, n, N, 0, S, d, qop, dop, tile, wave, kWaves, lane, sc, s_pad);
-        lds_barrier();
-        const int chunks = tile_chunks<FMT>(d);
-        for (int i = threadIdx.x; i < S; i += kBlock) {
-            const float rv = rsqrtf(chunk_sum(sc, s_pad, chunks, 1, i) * inv_d + eps);
-            const float dot = chunk_sum(sc, s_pad, chunks, 0, i), gi = chunk_sum(sc, s_pad, chunks, 2, i);
-            sc[i] = dot * rv;
-            ri[i] = rv;
-            g[i] = gi;
+        if constexpr (TILES) {
+            make_operand(dH + (size_t)n * d, d, dop, threadIdx.x, kBlock);
+            lds_barrier();
+            tile_dots(codes, scales, n, N, 0, S, d, qop, dop, tile, wave, kWaves, lane, sc, s_pad);
+            lds_barrier();
+            const int chunks = tile_chunks(d);
+            for (int i = threadIdx.x; i < S; i += kBlock) {
+                const float rv = rsqrtf(chunk_sum(sc, s_pad, chunks, 1, i) * inv_d + eps);
+                const float dot = chunk_sum(sc, s_pad, chunks, 0, i);
+                const float gi = chunk_sum(sc, s_pad, chunks, 2, i);
+                sc[i] = dot * rv;
+                ri[i] = rv;
+                g[i] = gi;
+            }
+        } else {
+            constexpr int U = NCH >= 4 ? 4 : 8;  // sources a group in flight
+            const int i1 = wave * G + ln.g;      // its first; every GG-th follows
+            const size_t first = (size_t)n * ln.nu, plane = (size_t)N * ln.nu;
+            float dh[NCH][CW], qv[NCH][CW];
+            load_dh<FMT, T, LG, NCH>(dH + (size_t)n * d, ln, d, dh);
+#pragma unroll
+            for (int c = 0; c < NCH; ++c)
+#pragma unroll
+                for (int e = 0; e < CW; e += 4) {
+                    const f32x4_t x = *reinterpret_cast<const f32x4_t *>(ql + ln.col(c) + e);
+                    qv[c][e] = x.x; qv[c][e + 1] = x.y; qv[c][e + 2] = x.z; qv[c][e + 3] = x.w;
+                }
+            for (int i0 = 0; i0 < S; i0 += U * GG) {
+                UnitRaw<FMT> w[U][NCH];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const size_t b = min(i0 + u * GG + i1, S - 1) * plane + first;
+#pragma unroll
+                    for (int c = 0; c < NCH; ++c)
+                        load_unit<FMT>(codes + b * 16, scales + b / per, ln.at[c], w[u][c]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int v = 0; v < U; v += 4) {
+                    if (i0 + v * GG >= S)
+                        break;  // uniform
+                    float ss[4], dot[4], p[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        ss[u] = dot[u] = p[u] = 0.0f;
+#pragma unroll
+                        for (int c = 0; c < NCH; ++c) {
+                            float a = 0.0f;
+#pragma unroll
+                            for (int h = 0; h < CW / 16; ++h) {
+                                float x[16];
+                                unit_values<FMT>(w[v + u][c], h, x);
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) {
+                                    a = fmaf(x[e], x[e], a);
+                                    dot[u] = fmaf(qv[c][16 * h + e], x[e], dot[u]);
+                                    p[u] = fmaf(dh[c][16 * h + e], x[e], p[u]);
+                                }
+                            }
+                            ss[u] += ln.in[c] ? a : 0.0f;
+                        }
+                    }
+                    const float tss = four_sums<LG>(ss, lane), tdot = four_sums<LG>(dot, lane),
+                                tg = four_sums<LG>(p, lane);
+                    const int i = i0 + (v + four_index<LG>(lane)) * GG + i1;
+                    if (lane % (LG / 4) == 0 && i < S) {
+                        const float rv = rsqrtf(tss * inv_d + eps);
+                        ri[i] = rv;
+                        sc[i] = tdot * rv;
+                        g[i] = tg;
+                    }
+                }
+            }
         }
         lds_barrier();
         float m = -INFINITY, z = 0.0f, gb = 0.0f;
@@ -657,10 +732,11 @@ hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, 
         if (p.mode == LRAR_MODE_FULL) {
             constexpr int NO = value_chunks<T>(NCH * LG * unit_cols<FMT>());
             const int s4 = (S + 3) / 4 * 4;  // 16-byte aligned rows behind the scores
-            const size_t lds = ((size_t)(3 * tile_chunks<FMT>(d) + kWaves) * s4 + NO * (1024 / sizeof(T))) * sizeof(float) +
-                               2 * operand_bytes<FMT>(d) + kWaves * kTileBytes;
+            size_t lds = ((size_t)(full_parts<FMT>(d) + kWaves) * s4 + NO * (1024 / sizeof(T))) * sizeof(float);
+            if constexpr (FMT == LRAR_CACHE_FP4)
+                lds += 2 * operand_bytes(d) + kWaves * kTileBytes;
             auto launch = [&](auto add) {
-                hipLaunchKernelGGL((cache_bwd_full<FMT, T, NO, decltype(add)::value>), dim3(pl.nblocks),
+                hipLaunchKernelGGL((cache_bwd_full<FMT, T, LG, NCH, decltype(add)::value>), dim3(pl.nblocks),
                                    dim3(kBlock), lds, st, p.codes, p.scales, p.q, dh, dv, partial, S, N,
                                    d, p.eps, s4, pl.tpw);
             };

@@ -198,6 +198,8 @@ MANY = [
     ("projected", 5, 2053, 64, 8), ("projected", 3, 2500, 1000, 24), ("projected", 4, 4400, 40, 9),
     ("sliced", 4, 2051, 100, 19), ("sliced", 3, 2100, 1056, 64), ("sliced", 2, 4500, 33, 8),
     ("full", 4, 2061, 72, 72), ("full", 3, 2050, 1040, 1040), ("full", 3, 4200, 31, 31),
+    ("projected", 3, 8197, 33, 8), ("sliced", 2, 8203, 1030, 16), ("full", 2, 8195, 40, 40),
+    ("projected", 2, 33001, 24, 4),
 ]
 IDS = [f"{m}_{S}x{N}x{d}_r{r}" for m, S, N, d, r in SITES + MANY]
 
@@ -263,6 +265,17 @@ def test_wide_forward(dev, d, r):
             N = 5
         p = Problem(dev, "sliced", "fp8", "f32", 4, N, d, r)
         check("h", host(p.fwd()), p.site(False).h())
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_most_on_chip_memory(dev, fmt):
+    """The most sources, the widest rows and the narrowest (the most tokens a wave)."""
+    for mode, S, N, d, r in (("full", 512, 2, 4096, 4096), ("full", 512, 3, 40, 40),
+                             ("sliced", 512, 3, 70, 20), ("projected", 500, 1026, 20, 8)):
+        p = Problem(dev, mode, fmt, "f32", S, N, d, r)
+        site = p.site()
+        check("h", host(p.fwd()), site.h())
+        check_grads(p, p.bwd(), site)
 
 
 def test_most_sources(dev):
