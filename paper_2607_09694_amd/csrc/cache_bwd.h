@@ -384,12 +384,15 @@ cache_bwd_lr_wg(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ s
         UnitRaw<FMT> w[U][NCH];
         auto load = [&](int i0) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const size_t b = min(i0 + u * G + ln.g, ie - 1) * plane + first;
+            for (int h = 0; h < U; h += 4)
+                if (h == 0 || i0 + h * G < ie)  // wave-uniform
 #pragma unroll
-                for (int c = 0; c < NCH; ++c)
-                    load_unit<FMT>(codes + b * 16, scales + b / per_block, ln.at[c], w[u][c]);
-            }
+                    for (int u = h; u < h + 4; ++u) {
+                        const size_t b = min(i0 + u * G + ln.g, ie - 1) * plane + first;
+#pragma unroll
+                        for (int c = 0; c < NCH; ++c)
+                            load_unit<FMT>(codes + b * 16, scales + b / per_block, ln.at[c], w[u][c]);
+                    }
         };
         float dh[NCH][CW];
         load_dh<FMT, T, LG, NCH>(dhrow, ln, d, dh);
@@ -401,6 +404,8 @@ cache_bwd_lr_wg(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ s
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int h = 0; h < U; h += 4) {
+                if (h > 0 && i0 + h * G >= ie)
+                    break;
                 float p[4];
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {

@@ -232,15 +232,19 @@ cache_fwd_lr_wg(uint8_t *codes, uint8_t *scales, const void *__restrict__ K,
     float m = -INFINITY, l = 0.0f;
     if (ib < ie) {  // wave-uniform
         UnitRaw<FMT> w[U][NCH];
+        constexpr int B = U < 4 ? U : 4;  // sources a group that are skipped together
         auto load = [&](int i0) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const size_t b = min(i0 + u * G + ln.g, ie - 1) * plane + first;
+            for (int h = 0; h < U; h += B)
+                if (h == 0 || i0 + h * G < ie)  // wave-uniform
 #pragma unroll
-                for (int c = 0; c < NCH; ++c)
-                    load_unit<FMT>(codes + b * 16, scales + b / per_block,
-                                   (unsigned)min(c0 + ln.lu + c * LG, ln.nu - 1), w[u][c]);
-            }
+                    for (int u = h; u < h + B; ++u) {
+                        const size_t b = min(i0 + u * G + ln.g, ie - 1) * plane + first;
+#pragma unroll
+                        for (int c = 0; c < NCH; ++c)
+                            load_unit<FMT>(codes + b * 16, scales + b / per_block,
+                                           (unsigned)min(c0 + ln.lu + c * LG, ln.nu - 1), w[u][c]);
+                    }
         };
         if (o_new && ie == S) {
             // Group 0 stores the row; the loads below read it back.
@@ -286,6 +290,8 @@ cache_fwd_lr_wg(uint8_t *codes, uint8_t *scales, const void *__restrict__ K,
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                if (u > 0 && u % B == 0 && i0 + u * G >= ie)
+                    break;
                 const int i = i0 + u * G + ln.g;
                 const float a = i < ie ? s[min(i, ie - 1)] : 0.0f;
 #pragma unroll
