@@ -45,11 +45,10 @@ size_t lr_attnres_cache_row_scales(int64_t d);
  * Per block: e is the smallest of 1 .. 254 with max |x| <= M 2^(e - 127), M the
  * largest code (448 or 6), so nothing saturates; a code is x 2^(127 - e), an
  * exact product, rounded to nearest even.  A block that holds a NaN or an
- * infinity gets e = 255 and codes 0.  O needs element alignment (16 bytes and
- * d % 8 == 0 for the vector path).
+ * infinity gets e = 255 and codes 0.  O needs element alignment only.
  * EINVAL: rows < 0, d < 1, unknown format or storage, NULL or misaligned
  * pointers, overlapping buffers, a size overflowing int64.  EUNSUPPORTED:
- * rows above 2^40, d above 2^20.
+ * rows above 2^40, d above 2^20, more than about 2^31 workgroups' worth.
  */
 int lr_attnres_cache_write(const void *O, void *codes, void *scales, int64_t rows, int64_t d,
                            int format, int dtype, void *stream);
@@ -70,7 +69,7 @@ int lr_attnres_cache_read(const void *codes, const void *scales, void *O, int64_
  *       lr_attnres_cache_write, and the site reads that plane as every later
  *       site will.  With o_new NULL codes and scales are only read.
  * Errors as for lr_attnres_route_fwd, plus EINVAL for an unknown format.
- * EUNSUPPORTED: S > 1024, N > 2^30, full-rank keys with d > 4096, d > 2^20.
+ * EUNSUPPORTED: S > 1024, N > 2^25, full-rank keys with d > 4096, d > 2^20.
  */
 int lr_attnres_cache_route_fwd(void *codes, void *scales, const void *K, const float *q,
                                const void *o_new, void *H, int64_t S, int64_t N, int64_t d,
@@ -88,7 +87,7 @@ int lr_attnres_cache_route_fwd(void *codes, void *scales, const void *K, const f
  *   aligned (NULL when that is 0); what serves S sources serves fewer.
  * Results are bitwise reproducible.  Errors as for lr_attnres_route_bwd, plus
  * EINVAL for an unknown format and accumulate not 0 or 1.  EUNSUPPORTED:
- * S > 512, N > 2^30, projected or sliced keys with r > 256, d > 4096.
+ * S > 512, N > 2^25, projected or sliced keys with r > 256, d > 4096.
  */
 size_t lr_attnres_cache_route_bwd_workspace_bytes(int64_t S, int64_t N, int64_t d, int64_t r,
                                                   int mode, int format, int dtype);

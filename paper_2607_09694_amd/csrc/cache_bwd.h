@@ -8,7 +8,10 @@
 //     dq = sum ds_i k_i / rho_i,
 // the weights recomputed from the keys.  The stack is read once (full rank:
 // twice) in the units of a lane; dV, which does not depend on it beyond the key
-// columns, is written from dH alone in lanes of 8 columns, whole lines a wave.
+// columns, is written from dH alone, whole lines a store.  Bound by HBM: 64 sources,
+// 16384 tokens, d = 2048, e4m3, projected r = 32 takes 1090 us: 392 for the reads (5.8
+// TB/s), 664 for the 4.29 GB of dV (6.5 TB/s), 5 for dq.  The deferred form (49
+// sources, 16384 tokens, d = 1024, r = 16) reads at 6.2 TB/s, 145 us.
 #pragma once
 
 #include "cache_device.h"
@@ -233,7 +236,7 @@ __device__ __forceinline__ void store_coef(float *__restrict__ coef, const float
 // every group.  It writes the key gradients and the dq partials, and into coef the
 // coefficients or (gradient rows) the weights [S][N], from which
 // cache_value_grads writes the rest of dV: reads and writes of HBM in turn, not
-// mixed.
+// mixed (in one kernel the size above took 1380 us).
 template <int FMT, typename T, int LG, int NCH, bool SLICED, CacheGrad OUT, int TW>
 __global__ void __launch_bounds__(kBlock)
 cache_bwd_lr(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
@@ -333,7 +336,8 @@ cache_bwd_lr(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scal
 }
 
 // The value rows dV_i = alpha_i dH before column wend: a wave holds TT tokens' dH
-// and walks the planes.
+// and walks the planes, TT adjacent rows a plane (4.29 GB of d = 2048: one token 790
+// us, 4 760, 8 664).
 template <typename T, int NO, CacheGrad OUT, int TT>
 __global__ void __launch_bounds__(kBlock)
 cache_value_grads(const T *__restrict__ dH, const float *__restrict__ alpha, T *__restrict__ dV, int S,
@@ -717,10 +721,13 @@ struct CacheBwdPlan {
 };
 CacheBwdPlan cache_bwd_plan(const CacheProblem &p);
 
-// Workgroups that keep the write stream of the value rows busy.
+// Workgroups that keep the write stream of the value rows busy: from that many on
+// its waves take 8 tokens (e4m3, 49 sources, 8192 tokens, d = 1024, whole backward:
+// 224 us; with 2 tokens 244); with fewer tokens the sources are cut too.
 constexpr int kValueBlocks = 256;
-// Tokens a group of the low-rank backward where there are many, by chunks.
-constexpr int bwd_many(int nch) { return nch <= 2 ? 4 : 2; }
+// Tokens a group of the low-rank backward where there are many, by the columns
+// that its lanes hold (their dH stays in registers).
+constexpr int bwd_many(int64_t cols) { return cols <= 2048 ? 4 : 2; }
 
 template <int FMT, typename T>
 hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, void *dK,
@@ -786,7 +793,7 @@ hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, 
                                    st, p.codes, p.scales, p.K, p.q, dh, dv, dk, coef, partial, S, N,
                                    d, r, p.eps, s_pad, r_pad);
             else if (pl.many)
-                launch(std::integral_constant<int, bwd_many(NCH)>{});
+                launch(std::integral_constant<int, bwd_many(NCH * LG * unit_cols<FMT>())>{});
             else
                 launch(std::integral_constant<int, 1>{});
         };

@@ -13,17 +13,13 @@
 
 namespace lrar {
 
-constexpr int kCacheVec = 16;  // columns that a lane loads at once in the row streams
-
-// Codes of 16 and of 8 columns as one lane loads them.
+// Codes of 8 columns, and how they are packed.
 template <int FMT> struct Codes;
 template <> struct Codes<LRAR_CACHE_FP8> {
-    typedef u32x4_t row_t;
     typedef u32x2_t key_t;
     static constexpr int per_byte = 1;  // columns a byte
 };
 template <> struct Codes<LRAR_CACHE_FP4> {
-    typedef u32x2_t row_t;
     typedef unsigned key_t;
     static constexpr int per_byte = 2;
 };
@@ -278,8 +274,9 @@ template <int FMT, int LG, int NCH> struct Lanes {
     __device__ int col(int c) const { return (lu + c * LG) * unit_cols<FMT>(); }
 };
 
-// The units of a row of d columns; calls f(std::integral_constant<int, LG>,
-// std::integral_constant<int, NCH>) with the fewest lanes that hold a row.
+// Calls f(std::integral_constant<int, LG>, std::integral_constant<int, NCH>) with
+// the fewest lanes that hold a row of d columns (up to 4096; beyond, of one of its
+// column blocks).
 template <int FMT, typename F> hipError_t dispatch_lanes(int64_t d, F &&f)
 {
     typedef std::integral_constant<int, 64> L64;

@@ -4,7 +4,11 @@
 //
 // A lane takes 16 bytes of codes and one scale byte a source.  Decoding costs half
 // an instruction a column and the sum one, so the reads of the stack stay the
-// bound, as they are in bf16.
+// bound, as they are in bf16: 64 sources, 16384 tokens, d = 2048, e4m3, projected
+// r = 32 takes 352 us, 6.7 TB/s (a bf16 stack: 656 us).  Full-rank keys add two
+// products a column (|x|^2 and q . x) and the second decoding, and are bound by
+// them where the codes are small: 49 sources, 4096 tokens, d = 1024, e2m1 40 us,
+// of which the vector instructions are about 60%.
 #include "cache_device.h"
 
 namespace lrar {
@@ -115,7 +119,9 @@ __device__ __forceinline__ void add_unit(const UnitRaw<FMT> &w, float a, float (
 }  // namespace
 
 // Projected / sliced keys.  A wave owns the adjacent tokens of 64 / LG groups of
-// lanes, TW of them a group, whose rows are adjacent in every plane.  Grid x =
+// lanes, TW of them a group, whose rows are adjacent in every plane, and loads SB
+// sources of them a trip.  Long runs of adjacent rows read best: tokens x sources a
+// trip at the size above: 1 x 4 418 us, 2 x 1 391, 4 x 2 387, 4 x 1 370.  Grid x =
 // tokens, y = column blocks of NCH * LG units (each recomputes the cheap scores).
 template <int FMT, typename T, int LG, int NCH, bool SLICED, int TW, int SB>
 __global__ void __launch_bounds__(kBlock)
@@ -463,11 +469,19 @@ constexpr int64_t kMaxSourcesFwd = 1024, kMaxSourcesBwd = 512, kMaxRankBwd = 256
 constexpr int64_t kMaxRow = 4096;            // columns that a wave holds
 constexpr int64_t kMaxColumns = 1 << 20;     // of a row in column blocks
 
-// Tokens up to which a token's sources are split over a workgroup.
+// Tokens up to which a token's sources are split over a workgroup.  Split / one wave
+// a token: e4m3, 49 sources, d = 1024, r = 16: 700 tokens 11.6 / 13.5 us, 1024 tokens
+// 13.7 / 15.3, 1500 tokens 19.0 / 17.5; e2m1, 33 sources, sliced r = 64: 1024 tokens
+// 11.3 / 15.1, 1500 17.2 / 15.6; full rank, e2m1, 49 sources: 512 tokens 15 / 28, 2048
+// tokens 45 / 30.
 constexpr int64_t kSplitTokens = 1024;
 
 // Waves from which a wave of the low-rank forward takes several tokens a group
-// (two a SIMD), and the sources up to which their scores fit LDS.
+// (two a SIMD; their chain of trips is four times as long), and the sources up to
+// which their scores fit LDS.  One token / four: e4m3, 49 sources, d = 1024: 4099
+// tokens 42 / 55 us, 8192 tokens 77 / 71; 64 sources, d = 2048: 8192 tokens 192 / 180;
+// e2m1, 33 sources, d = 1024 (two tokens / eight a wave): 8192 tokens 36 / 56, 16384
+// tokens 68 / 70.
 constexpr int64_t kManyWaves = 2048, kManySources = 128;
 
 bool split_tokens(const CacheProblem &p) { return p.N <= kSplitTokens && p.S > 1; }
@@ -512,7 +526,7 @@ hipError_t launch_fwd_as(const CacheProblem &p, const void *o_new, void *H, hipS
                                        tokens * S * sizeof(float), st, codes, scales, p.K, p.q, h,
                                        S, N, d, r, p.eps, S);
                 };
-                constexpr int TWB = NCH >= 4 || LG == 16 ? 2 : 4;
+                constexpr int TWB = LG == 16 || cols > 2048 ? 2 : 4;  // (cols: registers)
                 if (N >= kManyWaves * G * TWB && S <= kManySources)
                     many(std::integral_constant<int, TWB>{}, std::integral_constant<int, LG == 16 ? 2 : 1>{});
                 else
@@ -531,8 +545,8 @@ hipError_t launch_fwd_as(const CacheProblem &p, const void *o_new, void *H, hipS
 
 int check_cache_supported(const CacheProblem &p, bool bwd, std::string *why)
 {
-    if (p.N > (1 << 30)) {
-        *why = "N exceeds 2^30 tokens";
+    if (p.N > (1 << 25)) {  // a launch's threads
+        *why = "N exceeds 2^25 tokens";
     } else if (p.S > (bwd ? kMaxSourcesBwd : kMaxSourcesFwd)) {
         *why = bwd ? "backward supports at most 512 sources" : "forward supports at most 1024 sources";
     } else if (bwd && p.mode != LRAR_MODE_FULL && p.r > kMaxRankBwd) {

@@ -9,13 +9,17 @@ namespace lrar {
 namespace {
 
 // Tokens up to which the low-rank backward splits each token's sources over a
-// workgroup.
+// workgroup.  Split / not, gradient rows: e4m3, 49 sources, d = 1024: 700 tokens 28 /
+// 38 us, 1001 tokens 36 / 43, 1500 tokens 56 / 56, 2500 tokens 90 / 81; e2m1, 30
+// sources, d = 512: 1001 tokens 24 / 35, 2500 tokens 50 / 43.  Deferred: e4m3, 49
+// sources: 600 tokens 19 / 22, 1001 tokens 20 / 22, 1500 tokens 27 / 24.
 constexpr int64_t kSplitBwd = 1024;
-// Waves from which a group takes several tokens (two a SIMD), and the sources up
-// to which their statistics fit LDS.
+// Waves from which a group takes several tokens (as in the forward), and the
+// sources up to which their statistics fit LDS.
 constexpr int64_t kManyWaves = 2048, kManySources = 128;
-// Workgroups from which one of full-rank keys takes several tokens in turn, for
-// fewer rows of dq partials.
+// Workgroups from which one of full-rank keys takes two or four tokens in turn, for
+// fewer rows of dq partials: e2m1, 49 x 2048 x 1024: four tokens 89 us, two 94, one 97
+// (the sum over the rows alone 5, 9 and 15).
 constexpr int64_t kFullBlocks = 512;
 
 }  // namespace
@@ -26,7 +30,7 @@ CacheBwdPlan cache_bwd_plan(const CacheProblem &p)
     const bool full = p.mode == LRAR_MODE_FULL;
     const int64_t units = cache_blocks(p.d) * (p.format == LRAR_CACHE_FP8 ? 2 : 1);
     const int64_t groups = units <= 16 ? 4 : units <= 32 ? 2 : 1;  // of lanes in a wave
-    const int many = bwd_many(units <= 64 ? 1 : units <= 128 ? 2 : 4);
+    const int many = bwd_many(p.d);
     pl.split = !full && p.N <= kSplitBwd;
     pl.many = !full && !pl.split && p.S <= kManySources && p.N >= kManyWaves * groups * many;
     pl.tpw = !full ? 1 : p.N >= 4 * kFullBlocks ? 4 : p.N >= 2 * kFullBlocks ? 2 : 1;

@@ -214,7 +214,7 @@ def test_backward_rejects(lib, call, name, kw, msg):
 
 def test_unsupported(lib):
     assert fwd(lib, S=1025) == EUNSUPPORTED
-    assert fwd(lib, N=(1 << 30) + 1, S=1, d=8, r=8) == EUNSUPPORTED
+    assert fwd(lib, N=(1 << 25) + 1, S=1, d=8, r=8) == EUNSUPPORTED
     assert fwd(lib, d=(1 << 20) + 1) == EUNSUPPORTED
     assert fwd(lib, mode=F, d=4097, r=4097) == EUNSUPPORTED
     for call in (bwd, deferred):

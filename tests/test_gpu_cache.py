@@ -199,7 +199,7 @@ MANY = [
     ("sliced", 4, 2051, 100, 19), ("sliced", 3, 2100, 1056, 64), ("sliced", 2, 4500, 33, 8),
     ("full", 4, 2061, 72, 72), ("full", 3, 2050, 1040, 1040), ("full", 3, 4200, 31, 31),
     ("projected", 3, 8197, 33, 8), ("sliced", 2, 8203, 1030, 16), ("full", 2, 8195, 40, 40),
-    ("projected", 2, 33001, 24, 4),
+    ("projected", 2, 33001, 24, 4), ("sliced", 2, 4099, 2300, 40),
 ]
 IDS = [f"{m}_{S}x{N}x{d}_r{r}" for m, S, N, d, r in SITES + MANY]
 
@@ -279,6 +279,8 @@ def test_most_on_chip_memory(dev, fmt):
 
 
 def test_most_sources(dev):
+    p = Problem(dev, "projected", "fp8", "bf16", 1024, 1030, 16, 4)
+    check("h", host(p.fwd()), p.site(False).h())
     p = Problem(dev, "projected", "fp4", "f32", 1024, 2, 64, 8)
     check("h", host(p.fwd()), p.site(False).h())
     p = Problem(dev, "sliced", "fp8", "bf16", 512, 3, 48, 16)
