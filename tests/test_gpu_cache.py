@@ -419,6 +419,45 @@ def test_other_stream(dev):
         assert (x is None and y is None) or torch.equal(x, y)
 
 
+def test_two_streams_at_once(dev):
+    """Calls in flight together, each with a workspace of its own."""
+    ps = [Problem(dev, m, f, "bf16", 30, 900, 520, 24) for m, f in
+          (("projected", "fp8"), ("sliced", "fp4"), ("full", "fp4"), ("full", "fp8"))]
+    want = [(p.fwd(), *p.bwd()) for p in ps]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ps]
+    got = [None] * len(ps)
+    for _ in range(3):
+        for k, (p, st) in enumerate(zip(ps, streams)):
+            with torch.cuda.stream(st):
+                got[k] = (p.fwd(), *p.bwd())
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        for x, y in zip(w, g):
+            assert (x is None and y is None) or torch.equal(x, y)
+
+
+def test_random_shapes(dev):
+    """Seeded shapes over the whole range, every call."""
+    rng = np.random.default_rng(77)
+    for k in range(60):
+        mode = ("projected", "sliced", "full")[k % 3]
+        fmt, dtype = FMTS[k // 3 % 2], ("bf16", "f32")[k // 6 % 2]
+        S = int(np.exp(rng.uniform(0, np.log(70))))
+        d = int(np.exp(rng.uniform(0, np.log(2500))))
+        N = min(int(np.exp(rng.uniform(0, np.log(9000)))), max(1, 1_500_000 // (S * d)))
+        r = min(d, int(np.exp(rng.uniform(0, np.log(256))))) if mode == "sliced" else \
+            int(np.exp(rng.uniform(0, np.log(256))))
+        p = Problem(dev, mode, fmt, dtype, S, N, d, r, seed=k)
+        site = p.site()
+        check("h", host(p.fwd()), site.h())
+        check_grads(p, p.bwd(), site)
+        if mode != "full":
+            coef, dq = p.deferred()
+            check("coef", host(coef), site.coef())
+            check("dq", host(dq), site.dq())
+
+
 def test_graph_replays(dev):
     """A decode step (append) and a backward in one captured graph, replayed with
     new inputs and eager work in between."""
