@@ -51,8 +51,8 @@ __device__ __forceinline__ void make_operand(const T *__restrict__ x, int d, uin
         top = max_magnitude(top, dpp_move<kDppXor2>(top));
         top = max_magnitude(top, dpp_move<kDppHalfMirror>(top));
         top = max_magnitude(top, dpp_move<kDppMirror>(top));
-        // The smallest e in 22 .. 254 with top <= 1.5 * 2^(e - 127): every digit has a
-        // scale byte of its own.
+        // The smallest e >= 22 with top <= 1.5 * 2^(e - 127): every digit has a scale
+        // byte of its own.  (255, above 1.5 * 2^127, reads as NaN, as infinities do.)
         const unsigned u = __float_as_uint(top);
         const int e2 = max((int)(u >> 23) + ((u & 0x7fffffu) > 0x400000u ? 1 : 0), 22);
         const bool bad = u >= 0x7f800000u;

@@ -586,3 +586,26 @@ def _gather_terms(sites, i, mode):
     if mode == "sliced":
         x[:, x.shape[1] - sites[0].r:] += _key_terms(sites, i)
     return x
+
+
+@pytest.mark.parametrize("mode", ["projected", "sliced", "full"])
+@pytest.mark.parametrize("S,N", [(5, 6), (35, 6), (5, 2100)])
+def test_nan_and_huge_values_in_4_bits_stay_with_their_token(dev, mode, S, N):
+    """As above over e2m1, whose full-rank dots of 16 sources share a product: a NaN
+    block, then (full rank) a gradient above 1.5 * 2^127, which counts as infinite."""
+    p = Problem(dev, mode, "fp4", "f32", S, N, 96, 16)
+    clean, grads = p.fwd(), p.bwd()
+    keep = torch.arange(N, device=dev) != 1
+    p.cache.scales[2, 1, 2] = 255
+    h, (dV, dK, dq) = p.fwd(), p.bwd()
+    assert torch.equal(h[keep], clean[keep])
+    assert torch.equal(dV[:, keep], grads[0][:, keep])
+    assert h[1, 64:].isnan().all() and dq.isnan().any()
+    if mode != "full":
+        return
+    assert h[1].isnan().all() and dV[:, 1].isnan().any()
+    p = Problem(dev, mode, "fp4", "f32", S, N, 96, 16)
+    p.dH[1, 40] = 3e38
+    dV, _, dq = p.bwd()
+    assert torch.equal(dV[:, keep], grads[0][:, keep])
+    assert not dV[:, 1].isfinite().all() and not dq.isfinite().all()
