@@ -253,6 +253,37 @@ __device__ __forceinline__ void unit_values(const UnitRaw<FMT> &w, int h, float 
     }
 }
 
+// use(a, i) for i = ib, ib + step, .. < ie (at least one), where load(a, i) reads what
+// it uses.  The next trip's loads are in flight over this one's arithmetic, in two
+// buffers in turn; a holds trip ib already.  Without / with: full-rank forward, e2m1,
+// 49 sources, d = 1024, 4096 tokens 40.9 / 36.1 us, 16384 tokens 142 / 122; sliced r =
+// 64, 33 x 4099 x 1024, e2m1, 25.5 / 22.8.
+template <typename B, typename L, typename U>
+__device__ __forceinline__ void pipelined(int ib, int ie, int step, B &a, L &&load, U &&use)
+{
+    B b;
+    int i = ib;
+    for (; i + 2 * step < ie; i += 2 * step) {
+        load(b, i + step);
+        __builtin_amdgcn_sched_barrier(0);
+        use(a, i);
+        __builtin_amdgcn_sched_barrier(0);
+        load(a, i + 2 * step);
+        __builtin_amdgcn_sched_barrier(0);
+        use(b, i + step);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (i + step < ie) {
+        load(b, i + step);
+        __builtin_amdgcn_sched_barrier(0);
+        use(a, i);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_memcpy(&a, &b, sizeof(B));
+        i += step;
+    }
+    use(a, i);
+}
+
 // Lane layout of the rows of d columns: units lu, lu + LG, .. (NCH of them) of the
 // rows of group g.  Lanes past the row re-read its last unit (in range; in[c] says
 // which units count).

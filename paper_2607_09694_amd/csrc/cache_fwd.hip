@@ -7,8 +7,8 @@
 // bound, as they are in bf16: 64 sources, 16384 tokens, d = 2048, e4m3, projected
 // r = 32 takes 352 us, 6.7 TB/s (a bf16 stack: 656 us).  Full-rank keys add two
 // products a column (|x|^2 and q . x) and the second decoding, and are bound by
-// them where the codes are small: 49 sources, 4096 tokens, d = 1024, e2m1 40 us,
-// of which the vector instructions are about 60%.
+// them where the codes are small: 49 sources, 4096 tokens, d = 1024, e2m1 36 us,
+// of which the vector instructions are about two thirds.
 #include "cache_device.h"
 
 namespace lrar {
@@ -149,8 +149,9 @@ cache_fwd_lr(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scal
             at[t][c] = (unsigned)((min(n0 + t * G + ln.g, N - 1) - n0) * ln.nu +
                                   min(c0 + ln.lu + c * LG, ln.nu - 1));
     const size_t first = (size_t)n0 * ln.nu, plane = (size_t)N * ln.nu;
-    UnitRaw<FMT> w[SB][TW][NCH];
-    auto load = [&](int i0) {
+    typedef UnitRaw<FMT> Trip[SB][TW][NCH];
+    Trip w;
+    auto load = [&](Trip &w, int i0) {
 #pragma unroll
         for (int u = 0; u < SB; ++u) {
             const size_t b = min(i0 + u, S - 1) * plane + first;
@@ -161,7 +162,7 @@ cache_fwd_lr(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scal
                     load_unit<FMT>(codes + b * 16, scales + b / per, at[t][c], w[u][t][c]);
         }
     };
-    load(0);  // does not depend on the scores: goes out before the keys' loads
+    load(w, 0);  // does not depend on the scores: goes out before the keys' loads
     cache_scores<FMT, T, SLICED, G * TW, G * TW <= 2 ? 4 : G * TW <= 4 ? 2 : 1>(
         Keys<FMT, T, SLICED>(K, codes, scales, N, d, r), q, 0, S, n0, eps, lane, s, nullptr, s_pad);
     wave_lds_sync();
@@ -177,10 +178,7 @@ cache_fwd_lr(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scal
 #pragma unroll
             for (int e = 0; e < CW; ++e)
                 acc[t][c][e] = 0.0f;
-    for (int i0 = 0; i0 < S; i0 += SB) {
-        if (i0 > 0)
-            load(i0);
-        __builtin_amdgcn_sched_barrier(0);
+    auto add = [&](const Trip &w, int i0) {
 #pragma unroll
         for (int u = 0; u < SB; ++u)
 #pragma unroll
@@ -190,7 +188,19 @@ cache_fwd_lr(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scal
                 for (int c = 0; c < NCH; ++c)
                     add_unit<FMT>(w[u][t][c], a, acc[t][c]);
             }
-        __builtin_amdgcn_sched_barrier(0);
+    };
+    // A wave of several tokens a group has loads enough in flight, and rows of more
+    // units no registers for a second buffer (e4m3, 20 x 3000 x 4000: 46 us, with it 55).
+    if constexpr (TW == 1 && NCH == 1) {
+        pipelined(0, S, SB, w, load, add);
+    } else {
+        for (int i0 = 0; i0 < S; i0 += SB) {
+            if (i0 > 0)
+                load(w, i0);
+            __builtin_amdgcn_sched_barrier(0);
+            add(w, i0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
 #pragma unroll
     for (int t = 0; t < TW; ++t) {
@@ -372,8 +382,8 @@ cache_fwd_full(uint8_t *codes, uint8_t *scales, const float *__restrict__ q,
     }
     const float inv_d = 1.0f / (float)d;
     float m = -INFINITY, l = 0.0f;
-    for (int i0 = ib; i0 < ie; i0 += 4 * step) {
-        UnitRaw<FMT> w[4][NCH];
+    typedef UnitRaw<FMT> Trip[4][NCH];
+    auto load = [&](Trip &w, int i0) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const size_t b = min(i0 + u * step + i1, ie - 1) * plane + first;
@@ -381,7 +391,8 @@ cache_fwd_full(uint8_t *codes, uint8_t *scales, const float *__restrict__ q,
             for (int c = 0; c < NCH; ++c)
                 load_unit<FMT>(codes + b * 16, scales + b / per_block, at[c], w[u][c]);
         }
-        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto add = [&](const Trip &w, int i0) {
         float ss[4], dot[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -430,6 +441,20 @@ cache_fwd_full(uint8_t *codes, uint8_t *scales, const float *__restrict__ q,
             for (int c = 0; c < NCH; ++c)
                 add_unit<FMT>(w[u][c], a, acc[c]);
         }
+    };
+    if constexpr (NCH == 1) {  // (more units: no registers for a second buffer)
+        if (ib < ie) {  // wave-uniform
+            Trip w;
+            load(w, ib);
+            pipelined(ib, ie, 4 * step, w, load, add);
+        }
+    } else {
+        for (int i0 = ib; i0 < ie; i0 += 4 * step) {
+            Trip w;
+            load(w, i0);
+            __builtin_amdgcn_sched_barrier(0);
+            add(w, i0);
+        }
     }
     if constexpr (W != 0) {
         if constexpr (G > 1) {  // the groups' states on one maximum
@@ -470,21 +495,25 @@ constexpr int64_t kMaxRow = 4096;            // columns that a wave holds
 constexpr int64_t kMaxColumns = 1 << 20;     // of a row in column blocks
 
 // Tokens up to which a token's sources are split over a workgroup.  Split / one wave
-// a token: e4m3, 49 sources, d = 1024, r = 16: 700 tokens 11.6 / 13.5 us, 1024 tokens
-// 13.7 / 15.3, 1500 tokens 19.0 / 17.5; e2m1, 33 sources, sliced r = 64: 1024 tokens
-// 11.3 / 15.1, 1500 17.2 / 15.6; full rank, e2m1, 49 sources: 512 tokens 15 / 28, 2048
-// tokens 45 / 30.
-constexpr int64_t kSplitTokens = 1024;
+// a token, 1024 tokens: e4m3, 64 sources, d = 2048 24.6 / 26.6 us, 49 sources, d =
+// 1024 13.3 / 12.0; e2m1, 33 sources, d = 500 10.6 / 17.1, d = 1024 11.5 / 11.8, at
+// 1500 tokens 15.9 / 12.5.  Full rank: e2m1, 49 sources, d = 1024: 512 tokens 14.1 /
+// 22.4, 700 tokens 19.9 / 22.6, 850 tokens 23.8 / 22.7; e4m3, 33 sources, d = 2048:
+// 700 tokens 25.0 / 23.0.
+constexpr int64_t kSplitTokens = 1024, kSplitFull = 768;
 
 // Waves from which a wave of the low-rank forward takes several tokens a group
 // (two a SIMD; their chain of trips is four times as long), and the sources up to
 // which their scores fit LDS.  One token / four: e4m3, 49 sources, d = 1024: 4099
-// tokens 42 / 55 us, 8192 tokens 77 / 71; 64 sources, d = 2048: 8192 tokens 192 / 180;
-// e2m1, 33 sources, d = 1024 (two tokens / eight a wave): 8192 tokens 36 / 56, 16384
-// tokens 68 / 70.
+// tokens 40 / 54 us, 8192 tokens 75 / 70; 64 sources, d = 2048: 8192 tokens 192 / 175;
+// e2m1, 33 sources, d = 1024 (two tokens / eight a wave): 8192 tokens 36 / 53, 16384
+// tokens 69 / 69; 64 sources, d = 2048: 9000 tokens 123 / 163, 16384 tokens 244 / 220.
 constexpr int64_t kManyWaves = 2048, kManySources = 128;
 
-bool split_tokens(const CacheProblem &p) { return p.N <= kSplitTokens && p.S > 1; }
+bool split_tokens(const CacheProblem &p)
+{
+    return p.N <= (p.mode == LRAR_MODE_FULL ? kSplitFull : kSplitTokens) && p.S > 1;
+}
 
 template <int FMT, typename T>
 hipError_t launch_fwd_as(const CacheProblem &p, const void *o_new, void *H, hipStream_t st)

@@ -609,3 +609,14 @@ def test_nan_and_huge_values_in_4_bits_stay_with_their_token(dev, mode, S, N):
     dV, _, dq = p.bwd()
     assert torch.equal(dV[:, keep], grads[0][:, keep])
     assert not dV[:, 1].isfinite().all() and not dq.isfinite().all()
+
+
+@pytest.mark.parametrize("mode,d,r", [("sliced", 40, 9), ("projected", 700, 16), ("full", 100, 100),
+                                      ("full", 700, 700)])
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("S", [1, 3, 4, 5, 8, 9, 12, 13, 16, 17, 20, 21, 41])
+def test_forward_of_every_number_of_trips(dev, mode, d, r, fmt, S):
+    """One wave a token, whose loads run ahead by a trip of four sources: no, one and
+    two buffers in use, odd and even numbers of trips, a last one that is not full."""
+    p = Problem(dev, mode, fmt, "bf16", S, 1030, d, r)
+    check("h", host(p.fwd()), p.site(grad=False).h())
