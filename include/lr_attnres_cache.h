@@ -85,9 +85,6 @@ int lr_attnres_cache_route_fwd(void *codes, void *scales, const void *K, const f
  *   `dtype`, dq [r] fp32; accumulate = 0 overwrites dV, dK and dq, 1 adds.
  *   workspace: lr_attnres_cache_route_bwd_workspace_bytes(...) bytes, 16-byte
  *   aligned (NULL when that is 0); what serves S sources serves fewer.
- * Full-rank keys over e2m1: q and dH enter their dots with the rows to 2^-22.5 of
- * the largest magnitude in a block of 32 columns, and magnitudes above 1.5 * 2^127
- * count as infinite there.
  * Results are bitwise reproducible.  Errors as for lr_attnres_route_bwd, plus
  * EINVAL for an unknown format and accumulate not 0 or 1.  EUNSUPPORTED:
  * S > 512, N > 2^25, projected or sliced keys with r > 256, d > 4096.

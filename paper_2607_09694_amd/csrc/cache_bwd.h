@@ -523,8 +523,8 @@ cache_bwd_full(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ sc
     float *alpha = lds + (parts + wave) * s_pad;    // a wave's own
     float *stage = lds + (parts + kWaves) * s_pad;  // [NO * 64 * VO]: q, at the end dq
     uint8_t *qop = reinterpret_cast<uint8_t *>(stage + NO * kWaveSize * VO);  // TILES: operands, tiles
-    uint8_t *dop = qop + operand_bytes(d);
-    uint8_t *tile = dop + operand_bytes(d) + wave * kTileBytes;
+    uint8_t *dop = qop + row_terms<float>() * term_bytes(d);
+    uint8_t *tile = dop + row_terms<T>() * term_bytes(d) + wave * kTileBytes;
     const float inv_d = 1.0f / (float)d;
     const int nb = (d + kCacheBlock - 1) / kCacheBlock;
     // The query in LDS: both passes read it in their own layout, and hold it only
@@ -549,7 +549,7 @@ cache_bwd_full(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ sc
         if constexpr (TILES) {
             make_operand(dH + (size_t)n * d, d, dop, threadIdx.x, kBlock);
             lds_barrier();
-            tile_dots(codes, scales, n, N, 0, S, d, qop, dop, tile, wave, kWaves, lane, sc, s_pad);
+            tile_dots<T>(codes, scales, n, N, 0, S, d, qop, tile, wave, kWaves, lane, sc, s_pad);
             lds_barrier();
             const int chunks = tile_chunks(d);
             for (int i = threadIdx.x; i < S; i += kBlock) {
@@ -746,7 +746,7 @@ hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, 
             const int s4 = (S + 3) / 4 * 4;  // 16-byte aligned rows behind the scores
             size_t lds = ((size_t)(full_parts<FMT>(d) + kWaves) * s4 + NO * (1024 / sizeof(T))) * sizeof(float);
             if constexpr (FMT == LRAR_CACHE_FP4)
-                lds += 2 * operand_bytes(d) + kWaves * kTileBytes;
+                lds += (row_terms<float>() + row_terms<T>()) * term_bytes(d) + kWaves * kTileBytes;
             auto launch = [&](auto add) {
                 hipLaunchKernelGGL((cache_bwd_full<FMT, T, LG, NCH, decltype(add)::value>), dim3(pl.nblocks),
                                    dim3(kBlock), lds, st, p.codes, p.scales, p.q, dh, dv, partial, S, N,

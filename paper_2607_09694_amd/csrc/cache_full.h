@@ -2,84 +2,72 @@
 // matrix cores (the key of source i is its whole row x_i): 16 sources of a token at
 // a time, q . x_i, |x_i|^2 (the diagonal of X X^T) and dH . x_i.
 //
-// e2m1 rows are operands as they lie in memory: a lane of the 16 x 16 x 128 product
-// holds one block of 32 columns and its scale.  q and dH enter as sums of 8 e2m1
-// digits -4 .. 3 (times 1/2), each block of 32 on one power of two, 2^-3 smaller
-// from digit to digit: off by at most 2^-22.5 of the block's largest magnitude, about
-// what the fp32 rounding of each product and sum is.  (dH is split anew for every
-// token: the digits of a column are formed together, in one integer.)  Digits times
-// codes are small integers, so the products are exact.
-// Not taken: e4m3 rows against such digits, because the 8-bit product of the matrix
-// cores aligns its terms to about 13 bits (measured 2e-4 of the sum of magnitudes);
-// e4m3 rows decoded to bf16 against three bf16 terms, exact, but slower than vector
-// code where the operands' on-chip memory leaves few waves (33 sources, 8192 tokens,
-// d = 2048: 672 us against 514; d = 1024, 49 x 2048: 103 against 112); and the
-// forward's scores, whose vector code reads the rows once (49 x 16384 x 1024, e2m1:
-// 144 us against 176).
+// Everything is exact before fp32 sums: an e2m1 value with its block's power of two is
+// a bf16 number (checked over every code and scale byte, subnormal ones included), and
+// q and fp32 dH enter as three bf16 terms, the leading 8, the next 8 and the last 8 bits
+// of every element on its own (bf16 dH as it is).  No element costs another its bits,
+// whatever range a block has.
+// Not taken: digits of q and dH on one power of two a block, which need no decoding but
+// lose what is 2^-24 of a block's largest element; e4m3 rows against the same bf16 terms,
+// slower than vector code where the operands' on-chip memory leaves few waves (33
+// sources, 8192 tokens, d = 2048: 672 us against 514; d = 1024, 49 x 2048: 103 against
+// 112); the 8-bit product of the matrix cores, which aligns its terms to about 13 bits
+// (measured 2e-4 of the sum of magnitudes); and the forward's scores, whose vector code
+// reads the rows once (49 x 16384 x 1024, e2m1: 144 us against 176).
 #pragma once
 
 #include "cache_device.h"
 
 namespace lrar {
 
-typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
-constexpr int kDigits = 8;      // e2m1 digits of a value
 constexpr int kTileRows = 16;   // sources of a tile
 
-// Bytes of LDS for one row operand (q or dH): the digits and an exponent of every
-// block, the row padded to whole steps of the product.
-constexpr int operand_bytes(int d) { return (d + 127) / 128 * 4 * (kDigits * 16 + 4); }
+// bf16 terms of an element of fp32 or storage T.
+template <typename T> constexpr int row_terms() { return sizeof(T) == 2 ? 1 : 3; }
+// Bytes of LDS for one term of a row operand (q or dH), the row padded to whole steps of
+// 128 columns.  (16 bytes more: the terms that a load reads together lie in other banks.)
+constexpr int term_bytes(int d) { return (d + 127) / 128 * 256 + 16; }
 
-// Row x [d] (fp32 or storage T) as an operand in LDS, by `threads` threads (a
-// multiple of 16).  The caller puts barriers around it.
+// Row x [d] (fp32 or storage T) as row_terms<T>() rows of bf16 in LDS, zeros past d, by
+// `threads` threads.  The terms are cut off, not rounded, so that none is larger than the
+// element; an infinity or NaN is its first term.  The caller puts barriers around it.
 template <typename T>
 __device__ __forceinline__ void make_operand(const T *__restrict__ x, int d, uint8_t *__restrict__ lds,
                                              int thread, int threads)
 {
-    const int nb = (d + 127) / 128 * 4;
-    int *scale = reinterpret_cast<int *>(lds + nb * kDigits * 16);
-    // Two neighbouring columns a thread, 16 threads a block.
-    for (int k = thread; k < nb * 16; k += threads) {
-        const int b = k / 16, col = 2 * k;
+    const int pairs = (d + 127) / 128 * 64, tb = term_bytes(d);
+    for (int k = thread; k < pairs; k += threads) {
         float y[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-            y[e] = col + e < d ? load_elem(x + col + e) : 0.0f;
-        float top = max_magnitude(max_magnitude(0.0f, y[0]), y[1]);
-        top = max_magnitude(top, dpp_move<kDppXor1>(top));
-        top = max_magnitude(top, dpp_move<kDppXor2>(top));
-        top = max_magnitude(top, dpp_move<kDppHalfMirror>(top));
-        top = max_magnitude(top, dpp_move<kDppMirror>(top));
-        // The smallest e >= 22 with top <= 1.5 * 2^(e - 127): every digit has a scale
-        // byte of its own.  (255, above 1.5 * 2^127, reads as NaN, as infinities do.)
-        const unsigned u = __float_as_uint(top);
-        const int e2 = max((int)(u >> 23) + ((u & 0x7fffffu) > 0x400000u ? 1 : 0), 22);
-        const bool bad = u >= 0x7f800000u;
-        if (k % 16 == 0)
-            scale[b] = bad ? 255 : e2;
-        unsigned w[2];
+            y[e] = 2 * k + e < d ? load_elem(x + 2 * k + e) : 0.0f;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            // In units of the last digit, |n| <= 3 * 8^7; plus 4 in every digit,
-            // the octal digits are 0 .. 7.
-            const int n = (int)rintf(ldexpf(bad ? 0.0f : y[e], 128 + 21 - e2));
-            unsigned v = (unsigned)(n + 0x924924);
-            v = (v & 0xfffu) | (v & 0xfff000u) << 4;  // a digit every 4 bits
-            v = (v & 0x003f003fu) | (v & 0x0fc00fc0u) << 2;
-            v = (v & 0x07070707u) | (v & 0x38383838u) << 1;
-            // Digit - 4 as sign and magnitude: 4 .. 7 are 0 .. 3, and 0 .. 3 the codes 12 .. 9.
-            const unsigned m = v & 0x33333333u, neg = (~v >> 2 & 0x11111111u) * 15u;
-            w[e] = (m & ~neg) | ((0xccccccccu & neg) - (m & neg));
+        for (int t = 0; t < row_terms<T>(); ++t) {
+            unsigned w[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const unsigned u = __float_as_uint(y[e]);
+                // (A NaN stays one without its last 16 bits.)
+                w[e] = (u & 0x7fffffffu) > 0x7f800000u ? 0x7fc00000u : u & 0xffff0000u;
+                const bool last = (u & 0x7f800000u) == 0x7f800000u;
+                y[e] = last ? 0.0f : y[e] - __uint_as_float(w[e]);
+            }
+            *reinterpret_cast<unsigned *>(lds + t * tb + 4 * k) = w[0] >> 16 | w[1];
         }
-        // Digit p of both columns in a byte, the largest digit first.
-        const unsigned even = (w[0] & 0x0f0f0f0fu) | (w[1] & 0x0f0f0f0fu) << 4;
-        const unsigned odd = (w[0] >> 4 & 0x0f0f0f0fu) | (w[1] & 0xf0f0f0f0u);
-#pragma unroll
-        for (int p = 0; p < kDigits; ++p)
-            lds[(b * kDigits + p) * 16 + k % 16] =
-                (uint8_t)(((7 - p) % 2 ? odd : even) >> 8 * ((7 - p) / 2));
     }
+}
+
+// 8 e2m1 codes of a word as bf16, times the block's scale.
+__device__ __forceinline__ bf16x8_t decode_bf16(unsigned w, float sc)
+{
+    const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 0);
+    const bf16x2_t b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 1);
+    const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 2);
+    const bf16x2_t e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 3);
+    return bf16x8_t{a.x, a.y, b.x, b.y, c.x, c.y, e.x, e.y};
 }
 
 // LDS of a wave for one tile: 16 rows of 512 bytes of codes (16 bytes of padding
@@ -93,14 +81,15 @@ constexpr int tile_chunks(int d) { return (d + kTileUnits * kCacheBlock - 1) / (
 // The dots of the sources [ib, ie) of the token whose rows are `row0` rows into
 // each plane, chunk by chunk of its columns: part[(3 c + 0, 1, 2) stride + i] takes
 // q . x_i, |x_i|^2 and dH . x_i over chunk c.  The (tile of 16 sources, chunk) pairs
-// are dealt to `waves` waves, this one being `wave`.  ql, dl: operands of q and dH;
-// tile: the wave's kTileBytes.  The rows come through LDS, the next pair's loads in
+// are dealt to `waves` waves, this one being `wave`.  op: the terms of q, then those of
+// dH; tile: the wave's kTileBytes.  The rows come through LDS, the next pair's loads in
 // flight over this one's products: read straight into the operands' layout, a load
-// touches 16 planes, and the backward took 77 us instead of 68 (49 x 2048 x 1024).
+// touches 16 planes, and the backward took 77 us instead of 68 (49 x 2048 x 1024, with
+// rows that needed no decoding; with it 68.7).
+template <typename T>
 __device__ __forceinline__ void tile_dots(const uint8_t *codes, const uint8_t *scales, size_t row0,
-                                          size_t plane,
-                                          int ib, int ie, int d, const uint8_t *__restrict__ ql,
-                                          const uint8_t *__restrict__ dl, uint8_t *tile, int wave,
+                                          size_t plane, int ib, int ie, int d,
+                                          const uint8_t *__restrict__ op, uint8_t *tile, int wave,
                                           int waves, int lane, float *part, int stride)
 {
     const int c = lane % 16, gr = lane / 16;
@@ -138,25 +127,23 @@ __device__ __forceinline__ void tile_dots(const uint8_t *codes, const uint8_t *s
             load(job + waves);
         wave_lds_sync();
         const int steps = (min(kTileUnits, nu - u0) + 3) / 4;  // 4 units of every row a step
-        const int nbp = (nu + 3) / 4 * 4;
-        // Columns 0 .. 7 of the product take q's digits, 8 .. 15 dH's.
-        const uint8_t *bl = c >= kDigits ? dl : ql;
-        const int *bs = reinterpret_cast<const int *>(bl + nbp * kDigits * 16);
+        // Columns 0, 1, 2 of the product take q's terms, 8 on dH's; the others repeat q's
+        // first and are not used.
+        const int qt = row_terms<float>(), dt = row_terms<T>();
+        const bool used = c % 8 < (c < 8 ? qt : dt);
+        const uint8_t *bl = op + (used ? c % 8 + (c < 8 ? 0 : qt) : 0) * term_bytes(d);
         for (int s = 0; s < steps; ++s) {
+            // Lane group gr has block 4 s + gr, 8 of its columns a product.
             const u32x4_t a = *reinterpret_cast<const u32x4_t *>(tile + c * kTileRow + (4 * s + gr) * 16);
-            const int ex = tscale[c * kTileScales + 4 * s + gr];
-            const int b = u0 + 4 * s + gr;
-            const u32x4_t qd = *reinterpret_cast<const u32x4_t *>(bl + (b * kDigits + c % kDigits) * 16);
-            const int qe = bs[b];
-            i32x8_t x = {0, 0, 0, 0, 0, 0, 0, 0}, y = x;
+            const float sc = block_scale(tscale[c * kTileScales + 4 * s + gr]);
+            const uint8_t *b = bl + (u0 + 4 * s + gr) * (2 * kCacheBlock);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                x[k] = (int)a[k];
-                y[k] = (int)qd[k];
+                const bf16x8_t x = decode_bf16(a[k], sc);
+                const bf16x8_t y = *reinterpret_cast<const bf16x8_t *>(b + 16 * k);
+                dq = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, dq, 0, 0, 0);
+                dx = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, x, dx, 0, 0, 0);
             }
-            dq = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                x, y, dq, 4, 4, 0, ex, 0, qe == 255 ? 255 : qe - 3 * (c % kDigits));
-            dx = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, x, dx, 4, 4, 0, ex, 0, ex);
         }
         // Row 4 gr + k, column c of a product is element k of the lane.
         float *out = part + 3 * chunk * stride + i0;
@@ -164,7 +151,7 @@ __device__ __forceinline__ void tile_dots(const uint8_t *codes, const uint8_t *s
         for (int k = 0; k < 4; ++k) {
             const int i = 4 * gr + k;
             // Sums over aligned groups of 8 columns: q's in the first, dH's in the second.
-            const float v = group_sum(dq[k], 8);
+            const float v = group_sum(used ? dq[k] : 0.0f, 8);
             if (i0 + i < ie) {
                 if (c == 0)
                     out[i] = v;
