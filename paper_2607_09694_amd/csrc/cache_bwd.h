@@ -489,15 +489,15 @@ template <int FMT, int VO> struct OutCodes {
     }
 };
 
-// Rows of s_pad floats that hold the dots of a token's sources.
-template <int FMT> constexpr int full_parts(int d)
+// Full-rank dots on the matrix cores (cache_full.h has both sides measured).
+template <int FMT, int LG, int NCH> constexpr bool full_tiles()
 {
-    return FMT == LRAR_CACHE_FP4 ? 3 * tile_chunks(d) : 3;
+    return FMT == LRAR_CACHE_FP4 && NCH * LG * unit_cols<FMT>() <= kTileUnits * kCacheBlock;
 }
 
 // Full-rank keys: one token a workgroup at a time (tpw in turn).  Pass 1 forms
-// |x|^2, q.x and dH.x of its sources, which meet in LDS: e2m1 rows on the matrix
-// cores (tile_dots), e4m3 rows dealt to the waves' groups of lanes.  Pass 2 deals
+// |x|^2, q.x and dH.x of its sources, which meet in LDS: e2m1 rows of up to 1024
+// columns on the matrix cores (tile_dots), others dealt to the waves' groups of lanes.  Pass 2 deals
 // the sources to the waves, reads the rows again (from the L2) in the layout of the
 // gradient rows, whole lines a store, and writes
 //     dV_i = alpha_i dH + (ds_i / rho_i)(q - x_i s_i / (rho_i d)),
@@ -511,17 +511,15 @@ cache_bwd_full(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ sc
     constexpr int G = kWaveSize / LG, CW = unit_cols<FMT>(), GG = kWaves * G;
     constexpr int per = kCacheBlock / CW;  // units a block
     constexpr int VO = 16 / sizeof(T), NO = value_chunks<T>(NCH * LG * CW), B = NO >= 8 ? 2 : 4;
-    constexpr bool TILES = FMT == LRAR_CACHE_FP4;
+    constexpr bool TILES = full_tiles<FMT, LG, NCH>();
     extern __shared__ float lds[];
     const int lane = threadIdx.x & (kWaveSize - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWaveSize);
     const Lanes<FMT, LG, NCH> ln(lane, d);
-    // The scores, 1 / rho and dH.x of the sources (before that, of every chunk of
-    // columns q.x, |x|^2 and dH.x).
+    // The scores, 1 / rho and dH.x of the sources (before that q.x, |x|^2 and dH.x).
     float *sc = lds, *ri = sc + s_pad, *g = ri + s_pad;
-    const int parts = full_parts<FMT>(d);
-    float *alpha = lds + (parts + wave) * s_pad;    // a wave's own
-    float *stage = lds + (parts + kWaves) * s_pad;  // [NO * 64 * VO]: q, at the end dq
+    float *alpha = g + (1 + wave) * s_pad;    // a wave's own
+    float *stage = g + (1 + kWaves) * s_pad;  // [NO * 64 * VO]: q, at the end dq
     uint8_t *qop = reinterpret_cast<uint8_t *>(stage + NO * kWaveSize * VO);  // TILES: operands, tiles
     uint8_t *dop = qop + row_terms<float>() * term_bytes(d);
     uint8_t *tile = dop + row_terms<T>() * term_bytes(d) + wave * kTileBytes;
@@ -551,14 +549,10 @@ cache_bwd_full(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ sc
             lds_barrier();
             tile_dots<T>(codes, scales, n, N, 0, S, d, qop, tile, wave, kWaves, lane, sc, s_pad);
             lds_barrier();
-            const int chunks = tile_chunks(d);
             for (int i = threadIdx.x; i < S; i += kBlock) {
-                const float rv = rsqrtf(chunk_sum(sc, s_pad, chunks, 1, i) * inv_d + eps);
-                const float dot = chunk_sum(sc, s_pad, chunks, 0, i);
-                const float gi = chunk_sum(sc, s_pad, chunks, 2, i);
-                sc[i] = dot * rv;
+                const float rv = rsqrtf(ri[i] * inv_d + eps);
+                sc[i] *= rv;
                 ri[i] = rv;
-                g[i] = gi;
             }
         } else {
             constexpr int U = NCH >= 4 ? 4 : 8;  // sources a group in flight
@@ -744,8 +738,8 @@ hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, 
         if (p.mode == LRAR_MODE_FULL) {
             constexpr int NO = value_chunks<T>(NCH * LG * unit_cols<FMT>());
             const int s4 = (S + 3) / 4 * 4;  // 16-byte aligned rows behind the scores
-            size_t lds = ((size_t)(full_parts<FMT>(d) + kWaves) * s4 + NO * (1024 / sizeof(T))) * sizeof(float);
-            if constexpr (FMT == LRAR_CACHE_FP4)
+            size_t lds = ((size_t)(3 + kWaves) * s4 + NO * (1024 / sizeof(T))) * sizeof(float);
+            if constexpr (full_tiles<FMT, LG, NCH>())
                 lds += (row_terms<float>() + row_terms<T>()) * term_bytes(d) + kWaves * kTileBytes;
             auto launch = [&](auto add) {
                 hipLaunchKernelGGL((cache_bwd_full<FMT, T, LG, NCH, decltype(add)::value>), dim3(pl.nblocks),

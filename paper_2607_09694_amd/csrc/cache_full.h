@@ -13,7 +13,13 @@
 // sources, 8192 tokens, d = 2048: 672 us against 514; d = 1024, 49 x 2048: 103 against
 // 112); the 8-bit product of the matrix cores, which aligns its terms to about 13 bits
 // (measured 2e-4 of the sum of magnitudes); and the forward's scores, whose vector code
-// reads the rows once (49 x 16384 x 1024, e2m1: 144 us against 176).
+// reads the rows once (49 x 16384 x 1024, e2m1: 144 us against 176).  Rows of more than
+// 1024 columns take vector code too.  Matrix cores / vector code, the whole backward, e2m1:
+// 49 x 2048 x 1024 68.7 / 90.3 us, 33 x 4096 x 1000 120 / 142, 16 x 2048 x 1024 41.3 / 44.8,
+// 8 x 4096 x 1024 67.4 / 66.4, 1 x 4096 x 1024 61.0 / 58.6, 49 x 4096 x 512 80 / 122, 4 x
+// 4096 x 128 35.5 / 46.4; 33 x 4096 x 1088 260 / 189, 49 x 2048 x 1536 157 / 141, 33 x
+// 8192 x 2048 570 / 427, 8 x 4096 x 2048 156 / 98 (there the tile's registers leave one
+// wave a SIMD, and the operands in on-chip memory few workgroups).
 #pragma once
 
 #include "cache_device.h"
@@ -74,18 +80,16 @@ __device__ __forceinline__ bf16x8_t decode_bf16(unsigned w, float sc)
 // after each: no bank conflict) and 32 scale bytes each (and 4).
 constexpr int kTileRow = 512 + 16, kTileScales = 32 + 4;
 constexpr int kTileBytes = kTileRows * (kTileRow + kTileScales);
-constexpr int kTileUnits = 32;  // blocks of a row in a tile
-// Chunks of a row of d columns.
-constexpr int tile_chunks(int d) { return (d + kTileUnits * kCacheBlock - 1) / (kTileUnits * kCacheBlock); }
+constexpr int kTileUnits = 32;  // blocks of a row in a tile: the whole row
 
-// The dots of the sources [ib, ie) of the token whose rows are `row0` rows into
-// each plane, chunk by chunk of its columns: part[(3 c + 0, 1, 2) stride + i] takes
-// q . x_i, |x_i|^2 and dH . x_i over chunk c.  The (tile of 16 sources, chunk) pairs
-// are dealt to `waves` waves, this one being `wave`.  op: the terms of q, then those of
-// dH; tile: the wave's kTileBytes.  The rows come through LDS, the next pair's loads in
-// flight over this one's products: read straight into the operands' layout, a load
-// touches 16 planes, and the backward took 77 us instead of 68 (49 x 2048 x 1024, with
-// rows that needed no decoding; with it 68.7).
+// The dots of the sources [ib, ie) of the token whose rows, of up to 1024 columns, are
+// `row0` rows into each plane: part[i], part[stride + i] and part[2 stride + i] take
+// q . x_i, |x_i|^2 and dH . x_i.  The tiles of 16 sources are dealt to `waves` waves,
+// this one being `wave`.  op: the terms of q, then those of dH; tile: the wave's
+// kTileBytes.  The rows come through LDS, the next tile's loads in flight over this
+// one's products: read straight into the operands' layout, a load touches 16 planes, and
+// the backward took 77 us instead of 68 (49 x 2048 x 1024, with rows that needed no
+// decoding; with it 68.7).
 template <typename T>
 __device__ __forceinline__ void tile_dots(const uint8_t *codes, const uint8_t *scales, size_t row0,
                                           size_t plane, int ib, int ie, int d,
@@ -94,12 +98,12 @@ __device__ __forceinline__ void tile_dots(const uint8_t *codes, const uint8_t *s
 {
     const int c = lane % 16, gr = lane / 16;
     const int nu = (d + kCacheBlock - 1) / kCacheBlock;
-    const int chunks = tile_chunks(d), jobs = (ie - ib + kTileRows - 1) / kTileRows * chunks;
+    const int tiles = (ie - ib + kTileRows - 1) / kTileRows;
     uint8_t *tscale = tile + kTileRows * kTileRow;
     UnitRaw<LRAR_CACHE_FP4> w[kTileRows / 2];
-    auto load = [&](int job) {  // two rows an access
-        const int i0 = ib + job / chunks * kTileRows;
-        const unsigned un = (unsigned)min(job % chunks * kTileUnits + lane % kTileUnits, nu - 1);
+    const unsigned un = (unsigned)min(lane % kTileUnits, nu - 1);
+    auto load = [&](int k0) {  // two rows an access
+        const int i0 = ib + k0 * kTileRows;
 #pragma unroll
         for (int k = 0; k < kTileRows / 2; ++k) {
             const size_t row = (size_t)min(i0 + 2 * k + lane / kTileUnits, ie - 1) * plane + row0;
@@ -109,24 +113,24 @@ __device__ __forceinline__ void tile_dots(const uint8_t *codes, const uint8_t *s
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    if (wave < jobs)
+    if (wave < tiles)
         load(wave);
-    for (int job = wave; job < jobs; job += waves) {
-        const int i0 = ib + job / chunks * kTileRows, chunk = job % chunks, u0 = chunk * kTileUnits;
+    for (int k0 = wave; k0 < tiles; k0 += waves) {
+        const int i0 = ib + k0 * kTileRows;
         f32x4_t dq = {0, 0, 0, 0}, dx = {0, 0, 0, 0};
-        wave_lds_sync();  // the pair before this one has been read
+        wave_lds_sync();  // the tile before this one has been read
 #pragma unroll
         for (int k = 0; k < kTileRows / 2; ++k) {
             const int r = 2 * k + lane / kTileUnits;
-            const bool in = u0 + lane % kTileUnits < nu;  // units past the row are zeros
+            const bool in = lane % kTileUnits < nu;  // units past the row are zeros
             *reinterpret_cast<u32x4_t *>(tile + r * kTileRow + lane % kTileUnits * 16) =
                 in ? w[k].c : u32x4_t{0u, 0u, 0u, 0u};
             tscale[r * kTileScales + lane % kTileUnits] = (uint8_t)(in ? w[k].e : 127u);
         }
-        if (job + waves < jobs)
-            load(job + waves);
+        if (k0 + waves < tiles)
+            load(k0 + waves);
         wave_lds_sync();
-        const int steps = (min(kTileUnits, nu - u0) + 3) / 4;  // 4 units of every row a step
+        const int steps = (nu + 3) / 4;  // 4 units of every row a step
         // Columns 0, 1, 2 of the product take q's terms, 8 on dH's; the others repeat q's
         // first and are not used.
         const int qt = row_terms<float>(), dt = row_terms<T>();
@@ -136,7 +140,7 @@ __device__ __forceinline__ void tile_dots(const uint8_t *codes, const uint8_t *s
             // Lane group gr has block 4 s + gr, 8 of its columns a product.
             const u32x4_t a = *reinterpret_cast<const u32x4_t *>(tile + c * kTileRow + (4 * s + gr) * 16);
             const float sc = block_scale(tscale[c * kTileScales + 4 * s + gr]);
-            const uint8_t *b = bl + (u0 + 4 * s + gr) * (2 * kCacheBlock);
+            const uint8_t *b = bl + (4 * s + gr) * (2 * kCacheBlock);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const bf16x8_t x = decode_bf16(a[k], sc);
@@ -146,7 +150,7 @@ __device__ __forceinline__ void tile_dots(const uint8_t *codes, const uint8_t *s
             }
         }
         // Row 4 gr + k, column c of a product is element k of the lane.
-        float *out = part + 3 * chunk * stride + i0;
+        float *out = part + i0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int i = 4 * gr + k;
@@ -162,15 +166,6 @@ __device__ __forceinline__ void tile_dots(const uint8_t *codes, const uint8_t *s
             }
         }
     }
-}
-
-// Value `which` (0, 1, 2) of source i over all chunks, in their order.
-__device__ __forceinline__ float chunk_sum(const float *part, int stride, int chunks, int which, int i)
-{
-    float v = part[which * stride + i];
-    for (int c = 1; c < chunks; ++c)
-        v += part[(3 * c + which) * stride + i];
-    return v;
 }
 
 }  // namespace lrar
