@@ -294,7 +294,9 @@ cache_fwd_lr_wg(uint8_t *codes, uint8_t *scales, const void *__restrict__ K,
             m = fmaxf(m, s[i]);
         m = group_max(m, kWaveSize);
         for (int i = ib + lane; i < ie; i += kWaveSize) {
-            const float e = expf(s[i] - m);
+            // (A range may hold no score above -inf, and then weighs nothing beside the
+            // others; NaN stays NaN.)
+            const float e = s[i] == -INFINITY ? 0.0f : expf(s[i] - m);
             s[i] = e;
             l += e;
         }

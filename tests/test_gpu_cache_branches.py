@@ -172,3 +172,28 @@ def test_cancelling_scores(dev, mode, S, N, d, fmt, dtype):
     if K is not None:
         check("dK", host(dK), site.dK())
     check("dq", host(dq), site.dq())
+
+
+@pytest.mark.parametrize("fmt", ["fp8", "fp4"])
+@pytest.mark.parametrize("mode", ["projected", "sliced", "full"])
+@pytest.mark.parametrize("S,N,bad", [(8, 3, (0, 1)), (8, 3, (6, 7)), (9, 2, (2, 3, 4, 5, 6, 7, 8)),
+                                     (5, 1100, (0, 1, 2)), (64, 2, tuple(range(16)))])
+def test_scores_below_the_range(dev, mode, S, N, bad, fmt):
+    """q . k of a few sources is below fp32's range (-inf): they weigh nothing beside the
+    others, however a token's sources are split."""
+    rng = np.random.default_rng(S)
+    d = r = 64
+    V = rng.standard_normal((S, N, d))
+    K = k = None
+    q = rng.standard_normal(r) / 8
+    q[0] = 2.0 ** 90
+    keys = V
+    if mode == "projected":
+        keys = rng.standard_normal((S, N, r))
+    keys[..., :32] = 0.0
+    keys[list(bad), :, 0] = -2.0 ** 55  # |k|^2 and rho are in range
+    if mode == "projected":
+        K, k = stored(keys, "f32", dev)
+    cache, stack = filled(V, fmt, dev)
+    h = lr.cache_route_fwd(cache, K, torch.from_numpy(q.astype(np.float32)).to(dev), mode, dtype=torch.float32)
+    check("h", host(h), Site(stack, k, q.astype(np.float32), r, EPS, "f32").h())
