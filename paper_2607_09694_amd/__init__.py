@@ -786,6 +786,13 @@ FORMATS = {"fp8": FP8, "fp4": FP4}
 _CODE_BYTES = (32, 16)  # of a block of 32 columns
 
 
+def _format(fmt) -> int:
+    code = FORMATS.get(fmt) if isinstance(fmt, str) else int(fmt)
+    if code not in (FP8, FP4):
+        raise ValueError(f"unknown cache format {fmt!r}")
+    return code
+
+
 class SourceCache:
     """A stack of S sources of N rows and d columns held in blocks of 32 columns:
     codes [S, N, 32 nb] ("fp8", e4m3) or [S, N, 16 nb] ("fp4", e2m1, the even
@@ -799,9 +806,7 @@ class SourceCache:
     def __init__(self, codes, scales, d: int, fmt="fp8"):
         import torch
 
-        self.fmt = FORMATS[fmt] if isinstance(fmt, str) else int(fmt)
-        if self.fmt not in (FP8, FP4):
-            raise ValueError(f"unknown cache format {fmt}")
+        self.fmt = _format(fmt)
         nb = -(-d // 32)
         if d < 1 or codes.dim() != 3 or codes.shape[2] != nb * _CODE_BYTES[self.fmt] \
                 or tuple(scales.shape) != (codes.shape[0], codes.shape[1], nb):
@@ -832,7 +837,7 @@ def source_cache(S: int, N: int, d: int, fmt="fp8", device="cuda") -> SourceCach
     """An empty cache (all zeros) of S sources of N rows and d columns."""
     import torch
 
-    f = FORMATS[fmt] if isinstance(fmt, str) else int(fmt)
+    f = _format(fmt)
     nb = -(-d // 32)
     return SourceCache(torch.zeros((S, N, nb * _CODE_BYTES[f]), dtype=torch.uint8, device=device),
                        torch.ones((S, N, nb), dtype=torch.uint8, device=device), d, f)
@@ -855,6 +860,8 @@ def _on(t, name, index, dtype=None):
 def _cache_site(cache, K, q, mode):
     """Shapes of one read site over a cache: (S, N, d, r)."""
     S, N, d = cache._shape
+    if q.dim() != 1:
+        raise ValueError("q must have one dimension")
     if mode == PROJECTED:
         if K is None or K.dim() != 3 or K.shape[0] != S or K.shape[1] != N:
             raise ValueError("K must be [S, N, r] for projected keys")
@@ -863,7 +870,7 @@ def _cache_site(cache, K, q, mode):
         raise ValueError("K must be None unless keys are projected")
     else:
         r = q.shape[0]
-    if q.dim() != 1 or q.shape[0] != r:
+    if q.shape[0] != r:
         raise ValueError(f"q must have shape ({r},)")
     return S, N, d, r
 
@@ -963,10 +970,10 @@ def cache_route_bwd_workspace_bytes(S, N, d, r, mode, fmt, dtype) -> int:
     sources."""
     import torch
 
-    code = _BF16 if dtype == torch.bfloat16 else _F32
-    f = FORMATS[fmt] if isinstance(fmt, str) else int(fmt)
-    return load_library().lr_attnres_cache_route_bwd_workspace_bytes(S, N, d, r, _mode(mode), f,
-                                                                     code)
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"values must be bfloat16 or float32, got {dtype}")
+    return load_library().lr_attnres_cache_route_bwd_workspace_bytes(
+        S, N, d, r, _mode(mode), _format(fmt), _BF16 if dtype == torch.bfloat16 else _F32)
 
 
 def _cache_workspace(lib, dH, S, N, d, r, mode, fmt, code):
