@@ -34,8 +34,8 @@ extern "C" {
 
 enum { LRAR_CACHE_FP8 = 0, LRAR_CACHE_FP4 = 1 };
 
-/* Bytes of one row's codes and of its scales; 0 for d < 1 or an unknown
- * format. */
+/* Bytes of one row's codes and of its scales; 0 for d < 1, d > 2^20 or an
+ * unknown format. */
 size_t lr_attnres_cache_row_bytes(int64_t d, int format);
 size_t lr_attnres_cache_row_scales(int64_t d);
 
@@ -45,7 +45,9 @@ size_t lr_attnres_cache_row_scales(int64_t d);
  * Per block: e is the smallest of 1 .. 254 with max |x| <= M 2^(e - 127), M the
  * largest code (448 or 6), so nothing saturates; a code is x 2^(127 - e), an
  * exact product, rounded to nearest even.  A block that holds a NaN or an
- * infinity gets e = 255 and codes 0.  O needs element alignment only.
+ * infinity gets e = 255 and codes 0.  Magnitudes from (1 - 2^-5) 2^128 on (e2m1:
+ * (1 - 2^-3) 2^128) round to 2^128, which fp32 does not hold: they read as
+ * infinities.  O needs element alignment only.
  * EINVAL: rows < 0, d < 1, unknown format or storage, NULL or misaligned
  * pointers, overlapping buffers, a size overflowing int64.  EUNSUPPORTED:
  * rows above 2^40, d above 2^20, more than about 2^31 workgroups' worth.
@@ -69,7 +71,8 @@ int lr_attnres_cache_read(const void *codes, const void *scales, void *O, int64_
  *       lr_attnres_cache_write, and the site reads that plane as every later
  *       site will.  With o_new NULL codes and scales are only read.
  * Errors as for lr_attnres_route_fwd, plus EINVAL for an unknown format.
- * EUNSUPPORTED: S > 1024, N > 2^25, full-rank keys with d > 4096, d > 2^20.
+ * EUNSUPPORTED: S > 1024, N > 2^25, full-rank keys with d > 4096, d > 2^20,
+ * projected keys with r > 2^20.
  */
 int lr_attnres_cache_route_fwd(void *codes, void *scales, const void *K, const float *q,
                                const void *o_new, void *H, int64_t S, int64_t N, int64_t d,

@@ -905,7 +905,8 @@ def cache_write(cache, O):
     """Quantises O [S, N, d] bf16/fp32 into the cache's planes (one source as it
     is written: ``cache_write(cache.planes(i), o[None])``).  Per block of 32
     columns the power of two is the smallest for which nothing saturates; codes
-    round to nearest even; a block with a NaN or an infinity reads as NaN."""
+    round to nearest even; a block with a NaN or an infinity reads as NaN, and a
+    value that rounds to 2^128 as an infinity."""
     lib = load_library()
     _shaped(O, cache._shape, "O")
     S, N, d = cache._shape

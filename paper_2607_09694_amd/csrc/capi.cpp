@@ -1111,9 +1111,7 @@ int cache_bwd(const void *codes, const void *scales, const void *K, const float 
     const size_t need = lrar::cache_bwd_workspace_bytes(p);
     if (need > 0 && (!workspace || workspace_bytes < need))
         return fail(LRAR_EINVAL, "workspace too small: need " + std::to_string(need) + " bytes");
-    int64_t cf;
-    if (!mul_ok(S * N, 12, &cf))
-        return fail(LRAR_EINVAL, "tensor size overflows int64");
+    const int64_t cf = S * N * 12;  // (at most 512 * 2^25 rows)
     const Span outs[] = {span("dV", dV, z.v), span("dK", dK, z.k), span("coef", coef, cf),
                          span("dq", dq, r * 4), span("workspace", workspace, (int64_t)need)};
     const Span ins[] = {span("codes", codes, z.codes), span("scales", scales, z.scales),

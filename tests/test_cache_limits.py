@@ -1,7 +1,5 @@
 """What the calls over the 8- and 4-bit stack refuse before a device is touched: formats
 and storages that do not exist, by one kind of error each, and the documented limits."""
-import ctypes
-
 import pytest
 
 import paper_2607_09694_amd as lr
@@ -39,3 +37,16 @@ def test_query_of_no_dimension(lib):  # noqa: F811
     c = make()
     with pytest.raises(ValueError, match="q must"):
         lr.cache_route_fwd(c, None, torch.zeros(()), "sliced")
+
+
+def test_projected_key_width(lib):  # noqa: F811
+    far = dict(codes=1 << 58, scales=1 << 56, H=1 << 50, o_new=None)  # room for the keys
+    assert fwd(lib, mode=P, K=K, r=(1 << 20) + 1, S=2, N=1, q=1 << 55, **far) == EUNSUPPORTED
+    assert "key width" in err(lib)
+
+
+def test_row_sizes_of_rows_too_wide(lib):  # noqa: F811
+    assert lib.lr_attnres_cache_row_scales(1 << 20) == 1 << 15
+    assert lib.lr_attnres_cache_row_scales((1 << 20) + 1) == 0
+    assert lib.lr_attnres_cache_row_bytes((1 << 20) + 1, FP8) == 0
+    assert lib.lr_attnres_cache_row_bytes((1 << 20) + 1, FP4) == 0

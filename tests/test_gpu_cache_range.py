@@ -138,3 +138,22 @@ def test_largest_finite_gradient(dev, fmt, dtype):
     dH[1, 40] = 3.3e38
     p = Full(dev, fmt, dtype, V, rng.standard_normal(d) / 10, dH)
     check_grads(p, p.bwd(), p.site())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("fmt,first", [("fp8", 1 - 2.0 ** -5), ("fp4", 1 - 2.0 ** -3)])
+def test_sources_that_round_to_two_to_the_128(dev, fmt, first, dtype):
+    """The largest sources: those that round to 2^128 read as infinities, the one before
+    them as the code below."""
+    step = 2.0 ** (-24 if dtype == "f32" else -8)
+    x = np.full((1, 2, 64), 1.0)
+    x[0, 0, 3], x[0, 0, 40] = first * 2.0 ** 127 * 2, -(first - step) * 2.0 ** 127 * 2
+    x[0, 1, 9] = (first - step) * 2.0 ** 127 * 2
+    O, exact = stored(x, dtype, dev)
+    assert np.array_equal(exact, x)  # every input is a number of the storage
+    cache = lr.source_cache(1, 2, 64, fmt, dev)
+    lr.cache_write(cache, O)
+    got = host(lr.cache_read(cache, O.dtype))
+    below = (1 - 2.0 ** -4) * 2.0 ** 127 * 2 if fmt == "fp8" else 0.75 * 2.0 ** 127 * 2
+    assert got[0, 0, 3] == np.inf and got[0, 0, 40] == -below and got[0, 1, 9] == below
+    assert np.isfinite(np.delete(got.reshape(-1), 3)).all()
