@@ -774,8 +774,15 @@ hipError_t launch_cache_bwd_as(const CacheProblem &p, const void *dH, void *dV, 
                                            dim3(kBlock), 0, st, dh, coef, dv, S, N, d,
                                            SL ? (d - r) / 8 * 8 : d, per);
                     };
+                    // Adding, a wave's loads of one token's rows are enough on the way, and
+                    // more of them split the store stream: one token / two / the most,
+                    // e4m3, whole backward: 64 x 16384 x 2048 2213 / 2219 / 3375 us, 49 x
+                    // 8192 x 1024 428 / 410 / 656, 33 x 4096 x 1024 130 / 163 / -, 20 x
+                    // 3000 x 4000 255 / 341 / -; fp32, 30 x 8192 x 1024 492 / 447 / 728.
                     constexpr int TM = NO <= 4 ? 8 : 4;
-                    if (N >= kValueBlocks * kWaves * TM)
+                    if constexpr (OUT == kGradAdd)
+                        rows(std::integral_constant<int, 1>{});
+                    else if (N >= kValueBlocks * kWaves * TM)
                         rows(std::integral_constant<int, TM>{});
                     else
                         rows(std::integral_constant<int, 2>{});
