@@ -140,6 +140,15 @@ def test_largest_finite_gradient(dev, fmt, dtype):
     check_grads(p, p.bwd(), p.site())
 
 
+def test_most_sources_of_the_widest_matrix_rows(dev):
+    """The most on-chip memory that rows of up to 1024 columns take."""
+    rng = np.random.default_rng(6)
+    S, N, d = 512, 2, 1024
+    V, dH = rng.standard_normal((S, N, d)), rng.standard_normal((N, d))
+    p = Full(dev, "fp4", "f32", V, rng.standard_normal(d) / 32, dH)
+    check_grads(p, p.bwd(), p.site())
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("fmt,first", [("fp8", 1 - 2.0 ** -5), ("fp4", 1 - 2.0 ** -3)])
 def test_sources_that_round_to_two_to_the_128(dev, fmt, first, dtype):
