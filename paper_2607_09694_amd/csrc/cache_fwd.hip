@@ -5,7 +5,7 @@
 // A lane takes 16 bytes of codes and one scale byte a source.  Decoding costs half
 // an instruction a column and the sum one, so the reads of the stack stay the
 // bound, as they are in bf16: 64 sources, 16384 tokens, d = 2048, e4m3, projected
-// r = 32 takes 352 us, 6.7 TB/s (a bf16 stack: 656 us).  Full-rank keys add two
+// r = 32 takes 350 us, 6.7 TB/s (a bf16 stack: 656 us).  Full-rank keys add two
 // products a column (|x|^2 and q . x) and the second decoding, and are bound by
 // them where the codes are small: 49 sources, 4096 tokens, d = 1024, e2m1 36 us,
 // of which the vector instructions are about two thirds.
@@ -121,8 +121,9 @@ __device__ __forceinline__ void add_unit(const UnitRaw<FMT> &w, float a, float (
 // Projected / sliced keys.  A wave owns the adjacent tokens of 64 / LG groups of
 // lanes, TW of them a group, whose rows are adjacent in every plane, and loads SB
 // sources of them a trip.  Long runs of adjacent rows read best: tokens x sources a
-// trip at the size above: 1 x 4 418 us, 2 x 1 391, 4 x 2 387, 4 x 1 370.  Grid x =
-// tokens, y = column blocks of NCH * LG units (each recomputes the cheap scores).
+// trip at the size above, H's allocation included: 1 x 4 418 us, 2 x 1 391, 4 x 2
+// 387, 4 x 1 370.  Grid x = tokens, y = column blocks of NCH * LG units (each
+// recomputes the cheap scores).
 template <int FMT, typename T, int LG, int NCH, bool SLICED, int TW, int SB>
 __global__ void __launch_bounds__(kBlock)
 cache_fwd_lr(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
@@ -214,9 +215,9 @@ cache_fwd_lr(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scal
 // W ranges, whose online-softmax states meet in LDS.  The groups of a wave take
 // every G-th source of its range, U of them in flight a lane: what bounds a
 // launch of few tokens is the chain of dependent loads.
-// o_new: the newest source of every token (or NULL): the lanes that read source
-// S-1 quantise it from there, store it into plane S-1 and go on from registers.
-// (That plane is written here and read again by the scores: no restrict.)
+// o_new: the newest source of every token (or NULL): the wave whose range ends with
+// source S-1 quantises it from there, stores it into plane S-1 and reads it back with
+// the others.  (That plane is written here and read again: no restrict.)
 template <int FMT, typename T, int LG, int NCH, bool SLICED, int W>
 __global__ void __launch_bounds__(W * kWaveSize)
 cache_fwd_lr_wg(uint8_t *codes, uint8_t *scales, const void *__restrict__ K,
@@ -496,12 +497,13 @@ constexpr int64_t kMaxSourcesFwd = 1024, kMaxSourcesBwd = 512, kMaxRankBwd = 256
 constexpr int64_t kMaxRow = 4096;            // columns that a wave holds
 constexpr int64_t kMaxColumns = 1 << 20;     // of a row in column blocks
 
-// Tokens up to which a token's sources are split over a workgroup.  Split / one wave
-// a token, 1024 tokens: e4m3, 64 sources, d = 2048 24.6 / 26.6 us, 49 sources, d =
-// 1024 13.3 / 12.0; e2m1, 33 sources, d = 500 10.6 / 17.1, d = 1024 11.5 / 11.8, at
-// 1500 tokens 15.9 / 12.5.  Full rank: e2m1, 49 sources, d = 1024: 512 tokens 14.1 /
-// 22.4, 700 tokens 19.9 / 22.6, 850 tokens 23.8 / 22.7; e4m3, 33 sources, d = 2048:
-// 700 tokens 25.0 / 23.0.
+// Tokens up to which a token's sources are split over a workgroup: one number for all
+// widths, at which wide rows are about level; rows of few columns, several tokens of
+// which share a wave, would gain from more.  Split / one wave a token, 1024 tokens:
+// e4m3, 64 sources, d = 2048 24.6 / 26.6 us, 49 sources, d = 1024 13.3 / 12.0; e2m1, 33
+// sources, d = 500 10.6 / 17.1, d = 1024 11.5 / 11.8, at 1500 tokens 15.9 / 12.5.  Full
+// rank: e2m1, 49 sources, d = 1024: 512 tokens 14.1 / 22.4, 700 tokens 19.9 / 22.6, 850
+// tokens 23.8 / 22.7; e4m3, 33 sources, d = 2048: 700 tokens 25.0 / 23.0.
 constexpr int64_t kSplitTokens = 1024, kSplitFull = 768;
 
 // Waves from which a wave of the low-rank forward takes several tokens a group
